@@ -39,6 +39,9 @@ extern "C" {
 #define POWATTN_POWER  1u  /* attend block distances that are zero or a power of two (the power term of Algorithm 1) */
 #define POWATTN_DENSE  2u  /* full causal attention, A_i = {j <= i} (Section 3.1); other fields except block are ignored */
 
+/* powattn_qk_norm_rope flags */
+#define POWATTN_ROPE_INTERLEAVED 1u  /* pairs (2i, 2i+1) instead of (i, i + rot_dim/2) */
+
 /* element types of Q/K/V/O */
 #define POWATTN_BF16 0
 #define POWATTN_F32  1
@@ -379,6 +382,148 @@ int powattn_backward(const powattn_pattern* pattern,
                      int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int64_t seq_len,
                      int32_t head_dim, int32_t dtype, float softmax_scale,
                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- around the attention calls: pages and slots, norm and rotation, a cache of 4-bit floats ---- */
+
+/*
+ * Pages and slots of a serving step's new tokens, from the requests' lengths, on
+ * the GPU and in one launch (the block tables of powattn_prefill_batch_paged and
+ * the paged decode calls).  Sequence b has s = d_q_start[b] tokens in its
+ * pages and gets n = d_q_len[b] more; its new pages, ceil((s+n)/block) -
+ * ceil(s/block) of them, are taken from the head of the list of free pages,
+ * sequence 0's first, then sequence 1's and so on.
+ *   d_q_start, d_q_len  device int32 [batch]; clamped as by powattn_prefill_batch_paged: s into
+ *                     [0, table_stride*block], n into [0, min(q_rows, table_stride*block - s)]
+ *   d_free_pages      device int32 [n_free]: the free pages, in the order in which they are to be
+ *                     taken (may be null when n_free is 0)
+ *   d_block_table     device int32 [batch, table_stride], in and out: the entries of the new pages
+ *                     are written (-1 where the free list is too short), all others stay as they are
+ *   d_slots           device int32 [batch, q_rows], out: entry [b][r] is page * block + offset of position
+ *                     s + r, for powattn_cache_store_q4; -1 for r >= n and where the table's
+ *                     page is not in [0, n_pages)
+ *   d_kv_len          device int32 [batch], out: s + n, as the decode calls take it
+ *   d_n_taken         device int32 [1], out: the number of new pages of all sequences; more than n_free: the list was too short
+ * The free list itself is not changed: the pages taken are its first d_n_taken[0].  The inputs may not overlap the outputs.
+ * Limits: table_stride * block and n_pages * block below 2^31.
+ * Errors: INVALID_ARG (q_rows above table_stride*block among them), UNSUPPORTED, HIP_ERROR.
+ */
+int powattn_page_tables(const powattn_pattern* pattern, const int32_t* d_q_start, const int32_t* d_q_len,
+                        int32_t batch, int64_t q_rows, const int32_t* d_free_pages, int32_t n_free, int64_t n_pages,
+                        int32_t* d_block_table, int32_t table_stride,
+                        int32_t* d_slots, int32_t* d_kv_len, int32_t* d_n_taken, void* hip_stream);
+
+/*
+ * What models with normalised queries and keys do between the projections and the
+ * attention, in one pass: every query and key head is divided by its root mean
+ * square and multiplied by a weight, and its first rot_dim components are
+ * rotated by its position:
+ *   u = w * x / sqrt(mean(x^2) + eps);  (y_i, y_j) = (u_i cos a - u_j sin a, u_i sin a + u_j cos a),
+ *   a = position * inv_freq[p] for pair p = (i, j) = (p, p + rot_dim/2), or (2p, 2p+1) with POWATTN_ROPE_INTERLEAVED;
+ * components from rot_dim on are only normalised.  Computed in fp32 (the angles
+ * in fp64, so that far positions keep their digits), rounded once.
+ *   q, k              device rows [batch, heads, rows, head_dim] in any layout with contiguous components: strides
+ *                     holds the distances, in elements, between sequences, heads and rows (host int64 [3]),
+ *                     so that the projections' output [batch, rows, heads * head_dim] is taken as it is
+ *   q_weight, k_weight  device [head_dim], of the type of q and k
+ *   d_inv_freq        device float [rot_dim / 2] (may be null when rot_dim is 0)
+ *   rot_dim           a multiple of 16, 0 .. head_dim
+ *   d_q_start         device int32 [batch] or null (zeros): row r of sequence b is position d_q_start[b] + r
+ *   d_q_len           device int32 [batch] or null (all rows): rows r >= d_q_len[b] are neither read nor written
+ *   q_out, k_out      device [batch, n_q_heads, rows, head_dim], [batch, n_kv_heads, rows, head_dim], contiguous, as the
+ *                     attention calls take them; they may not overlap the inputs
+ *   dtype             POWATTN_BF16 or POWATTN_F32; head_dim 64 or 128
+ * Tensors and strides that are multiples of 16 bytes are read and written 16 bytes at a time.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP_ERROR.
+ */
+int powattn_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
+                         const void* q_weight, const void* k_weight, const float* d_inv_freq, int32_t rot_dim,
+                         uint32_t flags, const int32_t* d_q_start, const int32_t* d_q_len, void* q_out, void* k_out,
+                         int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int64_t rows, int32_t head_dim,
+                         int32_t dtype, float eps, void* hip_stream);
+
+/*
+ * Gradients of sum(q_out * d_q_out) + sum(k_out * d_k_out) of powattn_qk_norm_rope with the same inputs.
+ *   d_q_out, d_k_out  device, contiguous, as q_out and k_out (what powattn_backward writes as dq and dk)
+ *   dq, dk            device rows with strides of their own (host int64 [3]), so that they can be written into the gradient of
+ *                     the projections' output; no two rows may overlap.  Rows r >= d_q_len[b] are not written, and nothing
+ *                     of theirs is read
+ *   dq_weight, dk_weight  device float [head_dim], whatever dtype is: the sums over all rows and heads, in a fixed order
+ *   workspace         device, powattn_qk_norm_rope_backward_workspace_bytes(...) bytes, 256-byte aligned, contents ignored;
+ *                     calls that may run at the same time must not share one
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR.
+ */
+size_t powattn_qk_norm_rope_backward_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int64_t rows,
+                                                     int32_t head_dim);
+int powattn_qk_norm_rope_backward(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
+                                  const void* q_weight, const void* k_weight, const float* d_inv_freq, int32_t rot_dim,
+                                  uint32_t flags, const int32_t* d_q_start, const int32_t* d_q_len,
+                                  const void* d_q_out, const void* d_k_out,
+                                  void* dq, const int64_t* dq_strides, void* dk, const int64_t* dk_strides,
+                                  float* dq_weight, float* dk_weight,
+                                  int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int64_t rows, int32_t head_dim,
+                                  int32_t dtype, float eps, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The paged cache held in 4 bits: 0.27 of the bf16 cache's bytes.  A component is an e2m1 float (0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives), 32 consecutive components of a row share a power of two (e8m0: code c stands for 2^(c-127), 255 for
+ * NaN), as in the OCP microscaling format MXFP4.
+ *   k_pages, v_pages    device uint8 [n_pages, n_kv_heads, block, head_dim/2], 16-byte aligned: component 2i of a row in the
+ *                       low half of byte i, 2i+1 in the high half; a code is a sign bit and the index into the list above
+ *   k_scales, v_scales  device uint8 [n_pages, n_kv_heads, head_dim/32, block], 16-byte aligned: the scale codes (the token
+ *                       is the fastest index)
+ * powattn_cache_store_q4 writes rows of keys and values at their slots:
+ *   k, v                device bf16 rows [batch, n_kv_heads, rows, head_dim], strides in elements as for powattn_qk_norm_rope
+ *   d_slots             device int32 [batch, rows]: page * block + offset of row r of sequence b, as powattn_page_tables
+ *                       writes them; a row whose slot is outside [0, n_pages*block) is neither read nor stored.  No slot
+ *                       may occur twice in a call
+ * With m the largest magnitude of a group and 2^E <= m < 2^(E+1), the scale is 2^(E-2), or 2^(E-1) from m = 1.75 * 2^E on
+ * (which would round to 8), between 2^-127 and 2^125; the components are rounded to the nearest, ties to the even code,
+ * those beyond 6 to 6.  A group with an infinity or a NaN is stored as NaN.
+ *   dtype               POWATTN_BF16 only; head_dim 64 or 128; block a multiple of 64, at most 1024; n_pages * block < 2^31
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP_ERROR.
+ */
+int powattn_cache_store_q4(const powattn_pattern* pattern, const void* k, const int64_t* k_strides,
+                           const void* v, const int64_t* v_strides, const int32_t* d_slots,
+                           void* k_pages, void* v_pages, void* k_scales, void* v_scales, int64_t n_pages,
+                           int32_t batch, int32_t n_kv_heads, int64_t rows, int32_t head_dim, int32_t dtype,
+                           void* hip_stream);
+
+/*
+ * The rows of a 4-bit cache as bf16, exactly: for the prefill of a further piece of a prompt (powattn_prefill_chunk on the
+ * result), or to look at them.
+ *   d_block_table       device int32 [batch, table_stride]; a page number outside [0, n_pages) is clamped into the pool
+ *   d_start, d_length   device int32 [batch], or null (zeros, and all rows): row r of sequence b is position d_start[b] + r
+ *                       for r < d_length[b], both clamped so that they stay inside the table
+ *   k, v                device bf16 [batch, n_kv_heads, rows, head_dim], contiguous, 16-byte aligned; rows r >= d_length[b]
+ *                       (or beyond the table) are left as they were
+ * Everything else as for powattn_cache_store_q4.
+ */
+int powattn_cache_load_q4(const powattn_pattern* pattern, const void* k_pages, const void* v_pages,
+                          const void* k_scales, const void* v_scales, int64_t n_pages,
+                          const int32_t* d_block_table, int32_t table_stride,
+                          const int32_t* d_start, const int32_t* d_length, void* k, void* v,
+                          int32_t batch, int32_t n_kv_heads, int64_t rows, int32_t head_dim, int32_t dtype,
+                          void* hip_stream);
+
+/*
+ * powattn_decode_paged over the 4-bit cache: the result equals powattn_decode_paged on the bf16 pages that the cache stands
+ * for, up to rounding (the products of P and V keep 16 bits of P instead of 8).
+ *   q, o, lse, d_block_table, table_stride, softmax_scale   as for powattn_decode_paged; q 16-byte aligned
+ *   k_pages, v_pages, k_scales, v_scales, n_pages           as for powattn_cache_store_q4
+ *   d_kv_len            device int32 [batch], at most table_stride * block (clamped).  A sequence of 0 tokens or less (an
+ *                       idle place of a padded batch) attends nothing: its rows of o are zeros, of lse -inf
+ *   workspace           device, powattn_decode_paged_q4_workspace_bytes(..., table_stride * block) bytes, 256-byte aligned;
+ *                       needs no initialisation; calls that may run at the same time must not share one
+ * A row that attends a key without a number (a stored NaN) has none either.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR.
+ */
+size_t powattn_decode_paged_q4_workspace_bytes(const powattn_pattern* pattern, int32_t batch, int32_t n_q_heads,
+                                               int32_t n_kv_heads, int32_t head_dim, int64_t cache_capacity);
+int powattn_decode_paged_q4(const powattn_pattern* pattern, const void* q, const void* k_pages, const void* v_pages,
+                            const void* k_scales, const void* v_scales, int64_t n_pages,
+                            const int32_t* d_block_table, int32_t table_stride, const int32_t* d_kv_len,
+                            void* o, float* lse, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                            int32_t dtype, float softmax_scale, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

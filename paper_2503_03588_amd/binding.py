@@ -13,6 +13,7 @@ import operator
 import os
 import warnings
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -22,12 +23,16 @@ LIB_PATH = os.environ.get("POWATTN_LIB") or os.path.join(_HERE, "libpowattn.so")
 OK, INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR = 0, 1, 2, 3, 4
 POWER, DENSE = 1, 2
 BF16, F32 = 0, 1
+ROPE_INTERLEAVED = 1
 
 EXPORTS = (
     "powattn_version", "powattn_strerror", "powattn_num_blocks", "powattn_max_k",
     "powattn_row_host", "powattn_mask_build", "powattn_prefill",
     "powattn_prefill_chunk", "powattn_prefill_chunk_paged", "powattn_prefill_batch_paged", "powattn_prefill_varlen", "powattn_decode_workspace_bytes", "powattn_decode",
     "powattn_decode_static", "powattn_decode_paged", "powattn_backward_workspace_bytes", "powattn_backward",
+    "powattn_page_tables", "powattn_qk_norm_rope", "powattn_qk_norm_rope_backward_workspace_bytes",
+    "powattn_qk_norm_rope_backward", "powattn_cache_store_q4", "powattn_cache_load_q4",
+    "powattn_decode_paged_q4_workspace_bytes", "powattn_decode_paged_q4",
 )
 
 
@@ -161,6 +166,26 @@ def lib() -> ctypes.CDLL:
     L.powattn_backward.restype = ctypes.c_int
     L.powattn_backward.argtypes = [P, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i32, i32,
                                    f32, vp, ctypes.c_size_t, vp]
+    strides = ctypes.POINTER(i64)
+    L.powattn_page_tables.restype = ctypes.c_int
+    L.powattn_page_tables.argtypes = [P, vp, vp, i32, i64, vp, i32, i64, vp, i32, vp, vp, vp, vp]
+    L.powattn_qk_norm_rope.restype = ctypes.c_int
+    L.powattn_qk_norm_rope.argtypes = [vp, strides, vp, strides, vp, vp, vp, i32, ctypes.c_uint32, vp, vp, vp, vp, i32, i32, i32, i64,
+                                       i32, i32, f32, vp]
+    L.powattn_qk_norm_rope_backward_workspace_bytes.restype = ctypes.c_size_t
+    L.powattn_qk_norm_rope_backward_workspace_bytes.argtypes = [i32, i32, i32, i64, i32]
+    L.powattn_qk_norm_rope_backward.restype = ctypes.c_int
+    L.powattn_qk_norm_rope_backward.argtypes = [vp, strides, vp, strides, vp, vp, vp, i32, ctypes.c_uint32, vp, vp, vp, vp, vp, strides,
+                                                vp, strides, vp, vp, i32, i32, i32, i64, i32, i32, f32, vp, ctypes.c_size_t, vp]
+    L.powattn_cache_store_q4.restype = ctypes.c_int
+    L.powattn_cache_store_q4.argtypes = [P, vp, strides, vp, strides, vp, vp, vp, vp, vp, i64, i32, i32, i64, i32, i32, vp]
+    L.powattn_cache_load_q4.restype = ctypes.c_int
+    L.powattn_cache_load_q4.argtypes = [P, vp, vp, vp, vp, i64, vp, i32, vp, vp, vp, vp, i32, i32, i64, i32, i32, vp]
+    L.powattn_decode_paged_q4_workspace_bytes.restype = ctypes.c_size_t
+    L.powattn_decode_paged_q4_workspace_bytes.argtypes = [P, i32, i32, i32, i32, i64]
+    L.powattn_decode_paged_q4.restype = ctypes.c_int
+    L.powattn_decode_paged_q4.argtypes = [P, vp, vp, vp, vp, vp, i64, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, f32,
+                                          vp, ctypes.c_size_t, vp]
     _lib = L
     _native, _native_tried = None, False     # (the entry points' addresses are this library's)
     return L
@@ -561,4 +586,267 @@ def prefill_varlen(pattern: Pattern, kv_cnt, kv_idx, q, k, v, seq_lens, o=None, 
                                       _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), batch, hq, hkv, _ptr(seq_lens),
                                       npad, d, _dtype_code(q), float(softmax_scale), _stream(stream))
     _check(st, "powattn_prefill_varlen")
+    return o, lse
+
+
+# ---- around the attention calls ---------------------------------------------------------------------------------
+def _on_this_gpu(*tensors):
+    """The library enqueues on the current device's stream: a tensor elsewhere would be read by the wrong GPU."""
+    here = torch._C._cuda_getDevice() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError(f"tensors must be on the current GPU (cuda:{here}), not on {t.device}")
+
+
+def _int32(name, t, shape):
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous int32 {list(shape)}")
+
+
+def _output(name, t, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}")
+
+
+def _rows(name, t):
+    """The distances between sequences, heads and rows of [b,H,N,D] rows with contiguous components."""
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{name} must be [batch, heads, rows, head_dim] with contiguous components")
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def _rows_apart(name, t):
+    """... of a tensor that is written: no two rows may share memory."""
+    extent = t.shape[3]
+    for stride, size in sorted((t.stride(d), t.shape[d]) for d in range(3) if t.shape[d] > 1):
+        if stride < extent:
+            raise ValueError(f"{name}: rows overlap")
+        extent += stride * (size - 1)
+
+
+def page_tables(pattern: Pattern, q_start, q_len, free_pages, block_table, n_pages: int, q_rows: int, slots=None, kv_len=None,
+                n_taken=None, stream=None):
+    """powattn_page_tables.  q_start, q_len int32 [b]; free_pages int32 [n_free]; block_table int32 [b, table_stride], updated
+    in place.  Returns (slots int32 [b, q_rows], kv_len int32 [b], n_taken int32 [1])."""
+    batch = q_start.shape[0]
+    _int32("q_start", q_start, (batch,))
+    _int32("q_len", q_len, (batch,))
+    _int32("free_pages", free_pages, (free_pages.numel(),))
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be int32 [batch, table_stride]")
+    _int32("block_table", block_table, (batch, block_table.shape[1]))
+    if slots is None:
+        slots = torch.empty((batch, q_rows), dtype=torch.int32, device=q_start.device)
+    if kv_len is None:
+        kv_len = torch.empty((batch,), dtype=torch.int32, device=q_start.device)
+    if n_taken is None:
+        n_taken = torch.empty((1,), dtype=torch.int32, device=q_start.device)
+    _int32("slots", slots, (batch, q_rows))
+    _int32("kv_len", kv_len, (batch,))
+    _int32("n_taken", n_taken, (1,))
+    _on_this_gpu(q_start, q_len, free_pages, block_table, slots, kv_len, n_taken)
+    st = lib().powattn_page_tables(_pattern_ref(*pattern._values), _ptr(q_start), _ptr(q_len), batch, q_rows, _ptr(free_pages),
+                                   free_pages.numel(), n_pages, _ptr(block_table), block_table.shape[1], _ptr(slots),
+                                   _ptr(kv_len), _ptr(n_taken), _stream(stream))
+    _check(st, "powattn_page_tables")
+    return slots, kv_len, n_taken
+
+
+def _rope_arguments(q, k, q_weight, k_weight, inv_freq, q_start, q_len):
+    strides = _rows("q", q), _rows("k", k)
+    batch, hq, rows, d = q.shape
+    if k.shape != (batch, k.shape[1], rows, d):
+        raise ValueError("q/k shape mismatch")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w.dtype != q.dtype or w.shape != (d,) or not w.is_contiguous():
+            raise ValueError(f"{name} must be contiguous [head_dim] of the type of q")
+    if k.dtype != q.dtype:
+        raise ValueError("q/k dtype mismatch")
+    if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq must be contiguous float32 [rot_dim / 2]")
+    for name, t in (("q_start", q_start), ("q_len", q_len)):
+        if t is not None:
+            _int32(name, t, (batch,))
+    _on_this_gpu(q, k, q_weight, k_weight, inv_freq, q_start, q_len)
+    return strides, (batch, hq, k.shape[1], rows, d), 0 if inv_freq is None else 2 * inv_freq.numel()
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, q_start=None, q_len=None, eps=1e-6, interleaved=False, q_out=None, k_out=None,
+                 stream=None):
+    """powattn_qk_norm_rope.  q: [b,Hq,N,D], k: [b,Hkv,N,D], any strides with contiguous components (views of the projections'
+    output); weights [D]; inv_freq float32 [rot_dim / 2] or None (norm only); q_start, q_len int32 [b] or None.  Returns
+    contiguous (q_out, k_out); rows at or beyond a sequence's q_len are left as they were (zeros in outputs made here)."""
+    strides, (batch, hq, hkv, rows, d), rot = _rope_arguments(q, k, q_weight, k_weight, inv_freq, q_start, q_len)
+    new = torch.empty if q_len is None else torch.zeros
+    if q_out is None:
+        q_out = new((batch, hq, rows, d), dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = new((batch, hkv, rows, d), dtype=q.dtype, device=q.device)
+    _output("q_out", q_out, (batch, hq, rows, d), q.dtype)
+    _output("k_out", k_out, (batch, hkv, rows, d), q.dtype)
+    _on_this_gpu(q_out, k_out)
+    st = lib().powattn_qk_norm_rope(q.data_ptr(), strides[0], k.data_ptr(), strides[1], _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+                                    rot, ROPE_INTERLEAVED if interleaved else 0, _ptr(q_start), _ptr(q_len), _ptr(q_out),
+                                    _ptr(k_out), batch, hq, hkv, rows, d, _dtype_code(q), float(eps), _stream(stream))
+    _check(st, "powattn_qk_norm_rope")
+    return q_out, k_out
+
+
+def qk_norm_rope_backward_workspace_bytes(batch, n_q_heads, n_kv_heads, rows, head_dim) -> int:
+    return lib().powattn_qk_norm_rope_backward_workspace_bytes(batch, n_q_heads, n_kv_heads, rows, head_dim)
+
+
+def qk_norm_rope_backward_workspace(batch, n_q_heads, n_kv_heads, rows, head_dim, device="cuda"):
+    """An uninitialised workspace of the size powattn_qk_norm_rope_backward asks for."""
+    need = qk_norm_rope_backward_workspace_bytes(batch, n_q_heads, n_kv_heads, rows, head_dim)
+    if need == 0:
+        raise PowattnError(INVALID_ARG, "powattn_qk_norm_rope_backward_workspace_bytes")
+    return torch.empty((need,), dtype=torch.uint8, device=device)
+
+
+def qk_norm_rope_backward(q, k, q_weight, k_weight, inv_freq, dq_out, dk_out, q_start=None, q_len=None, eps=1e-6,
+                          interleaved=False, dq=None, dk=None, dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """powattn_qk_norm_rope_backward: the inputs of qk_norm_rope and the gradients of its outputs (contiguous).  dq, dk may have
+    strides of their own (views of the gradient of the projections' output).  Returns (dq, dk, dq_weight, dk_weight), the last
+    two float32 [D]; rows at or beyond a sequence's q_len are left as they were (zeros in gradients made here)."""
+    strides, (batch, hq, hkv, rows, d), rot = _rope_arguments(q, k, q_weight, k_weight, inv_freq, q_start, q_len)
+    _output("dq_out", dq_out, (batch, hq, rows, d), q.dtype)
+    _output("dk_out", dk_out, (batch, hkv, rows, d), q.dtype)
+    new = torch.empty if q_len is None else torch.zeros
+    if dq is None:
+        dq = new((batch, hq, rows, d), dtype=q.dtype, device=q.device)
+    if dk is None:
+        dk = new((batch, hkv, rows, d), dtype=q.dtype, device=q.device)
+    grad_strides = _rows("dq", dq), _rows("dk", dk)
+    if dq.shape != q.shape or dk.shape != k.shape or dq.dtype != q.dtype or dk.dtype != q.dtype:
+        raise ValueError("dq/dk must have the shapes and the type of q/k")
+    _rows_apart("dq", dq)
+    _rows_apart("dk", dk)
+    if dq_weight is None:
+        dq_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+    if dk_weight is None:
+        dk_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+    _output("dq_weight", dq_weight, (d,), torch.float32)
+    _output("dk_weight", dk_weight, (d,), torch.float32)
+    if workspace is None:
+        workspace = qk_norm_rope_backward_workspace(batch, hq, hkv, rows, d, q.device)
+    _on_this_gpu(dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace)
+    st = lib().powattn_qk_norm_rope_backward(
+        q.data_ptr(), strides[0], k.data_ptr(), strides[1], _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), rot,
+        ROPE_INTERLEAVED if interleaved else 0, _ptr(q_start), _ptr(q_len), _ptr(dq_out), _ptr(dk_out), dq.data_ptr(),
+        grad_strides[0], dk.data_ptr(), grad_strides[1], _ptr(dq_weight), _ptr(dk_weight), batch, hq, hkv, rows, d, _dtype_code(q),
+        float(eps), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "powattn_qk_norm_rope_backward")
+    return dq, dk, dq_weight, dk_weight
+
+
+class CacheQ4(NamedTuple):
+    """A paged cache held in 4 bits: k, v uint8 [n_pages, Hkv, block, D / 2] and their scale codes uint8
+    [n_pages, Hkv, D / 32, block] (the format: powattn_cache_store_q4).  The calls take any four tensors in this order."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def cache_q4(pattern: Pattern, n_pages, n_kv_heads, head_dim, device="cuda") -> CacheQ4:
+    """A cache of zeros."""
+    data, scale = (n_pages, n_kv_heads, pattern.block, head_dim // 2), (n_pages, n_kv_heads, head_dim // 32, pattern.block)
+    return CacheQ4(*(torch.zeros(shape, dtype=torch.uint8, device=device) for shape in (data, data, scale, scale)))
+
+
+def _cache_q4(pattern, cache, hkv, d):
+    """The four tensors' addresses, and the number of pages."""
+    k, v, ks, vs = cache
+    n_pages = k.shape[0]
+    for name, t, shape in (("k", k, (n_pages, hkv, pattern.block, d // 2)), ("v", v, (n_pages, hkv, pattern.block, d // 2)),
+                           ("k_scale", ks, (n_pages, hkv, d // 32, pattern.block)),
+                           ("v_scale", vs, (n_pages, hkv, d // 32, pattern.block))):
+        _output("cache." + name, t, shape, torch.uint8)
+    _on_this_gpu(k, v, ks, vs)
+    return (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()), n_pages
+
+
+def cache_store_q4(pattern: Pattern, k, v, cache, slots, stream=None):
+    """powattn_cache_store_q4.  k, v: bf16 [b,Hkv,N,D], any strides with contiguous components; slots int32 [b, N], as
+    page_tables gives them."""
+    strides = _rows("k", k), _rows("v", v)
+    batch, hkv, rows, d = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k/v must be alike")
+    _int32("slots", slots, (batch, rows))
+    pages, n_pages = _cache_q4(pattern, cache, hkv, d)
+    _on_this_gpu(k, v, slots)
+    st = lib().powattn_cache_store_q4(_pattern_ref(*pattern._values), k.data_ptr(), strides[0], v.data_ptr(), strides[1], _ptr(slots),
+                                      *pages, n_pages, batch, hkv, rows, d, _dtype_code(k), _stream(stream))
+    _check(st, "powattn_cache_store_q4")
+
+
+def cache_load_q4(pattern: Pattern, cache, block_table, rows: int, start=None, length=None, k=None, v=None, stream=None):
+    """powattn_cache_load_q4.  block_table int32 [b, table_stride]; start, length int32 [b] or None (zeros; all rows).
+    Returns (k, v), bf16 [b,Hkv,rows,D]: row r of sequence b is position start[b] + r; rows at or beyond length[b] are left as
+    they were (zeros in tensors made here)."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be int32 [batch, table_stride]")
+    batch, hkv, d = block_table.shape[0], cache[0].shape[1], 2 * cache[0].shape[3]
+    _int32("block_table", block_table, (batch, block_table.shape[1]))
+    for name, t in (("start", start), ("length", length)):
+        if t is not None:
+            _int32(name, t, (batch,))
+    pages, n_pages = _cache_q4(pattern, cache, hkv, d)
+    if k is None:
+        k = torch.zeros((batch, hkv, rows, d), dtype=torch.bfloat16, device=block_table.device)
+    if v is None:
+        v = torch.zeros((batch, hkv, rows, d), dtype=torch.bfloat16, device=block_table.device)
+    _output("k", k, (batch, hkv, rows, d), torch.bfloat16)
+    _output("v", v, (batch, hkv, rows, d), torch.bfloat16)
+    _on_this_gpu(block_table, start, length, k, v)
+    st = lib().powattn_cache_load_q4(_pattern_ref(*pattern._values), *pages, n_pages, _ptr(block_table), block_table.shape[1],
+                                     _ptr(start), _ptr(length), _ptr(k), _ptr(v), batch, hkv, rows, d, BF16, _stream(stream))
+    _check(st, "powattn_cache_load_q4")
+    return k, v
+
+
+def decode_paged_q4_workspace_bytes(pattern: Pattern, batch, n_q_heads, n_kv_heads, head_dim, cache_capacity) -> int:
+    return lib().powattn_decode_paged_q4_workspace_bytes(_pattern_ref(*pattern._values), batch, n_q_heads, n_kv_heads, head_dim,
+                                                         cache_capacity)
+
+
+def decode_paged_q4_workspace(pattern: Pattern, batch, n_q_heads, n_kv_heads, head_dim, cache_capacity, device="cuda"):
+    """An uninitialised workspace of the size powattn_decode_paged_q4 asks for (cache_capacity: table_stride * block)."""
+    need = decode_paged_q4_workspace_bytes(pattern, batch, n_q_heads, n_kv_heads, head_dim, cache_capacity)
+    if need == 0:
+        raise PowattnError(INVALID_ARG, "powattn_decode_paged_q4_workspace_bytes")
+    return torch.empty((need,), dtype=torch.uint8, device=device)
+
+
+def decode_paged_q4(pattern: Pattern, q, cache, block_table, kv_len, o=None, lse=None, softmax_scale=0.0, workspace=None,
+                    want_lse=True, stream=None):
+    """powattn_decode_paged_q4.  q/o: [b,Hq,D]; cache: a CacheQ4; block_table int32 [b, table_stride]; kv_len int32 [b]
+    (0: nothing is attended, o is zeros and lse -inf).  Returns (o, lse)."""
+    if q.dim() != 3 or not q.is_contiguous():
+        raise ValueError("q must be contiguous [batch, heads, head_dim]")
+    batch, hq, d = q.shape
+    hkv = cache[0].shape[1]
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be int32 [batch, table_stride]")
+    stride = block_table.shape[1]
+    _int32("block_table", block_table, (batch, stride))
+    _int32("kv_len", kv_len, (batch,))
+    pages, n_pages = _cache_q4(pattern, cache, hkv, d)
+    if o is None:
+        o = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty((batch, hq), dtype=torch.float32, device=q.device)
+    _output("o", o, q.shape, q.dtype)
+    if lse is not None:
+        _output("lse", lse, (batch, hq), torch.float32)
+    if workspace is None:
+        workspace = decode_paged_q4_workspace(pattern, batch, hq, hkv, d, stride * pattern.block, q.device)
+    _on_this_gpu(q, block_table, kv_len, o, lse, workspace)
+    st = lib().powattn_decode_paged_q4(_pattern_ref(*pattern._values), _ptr(q), *pages, n_pages, _ptr(block_table), stride,
+                                       _ptr(kv_len), _ptr(o), _ptr(lse), batch, hq, hkv, d, _dtype_code(q),
+                                       float(softmax_scale), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                       _stream(stream))
+    _check(st, "powattn_decode_paged_q4")
     return o, lse
