@@ -85,7 +85,8 @@ _native_tried = False
 HOST_PATH = os.path.join(_HERE, "_host.so")
 _NATIVE_ENTRY_POINTS = ("num_blocks", "max_k", "mask_build", "prefill", "prefill_chunk", "prefill_chunk_paged",
                         "prefill_batch_paged", "prefill_varlen", "decode", "decode_paged", "backward_workspace_bytes",
-                        "backward")
+                        "backward", "page_tables", "qk_norm_rope", "qk_norm_rope_backward", "cache_store_q4", "cache_load_q4",
+                        "decode_paged_q4")
 
 
 def _enable_native():
@@ -628,6 +629,10 @@ def page_tables(pattern: Pattern, q_start, q_len, free_pages, block_table, n_pag
                 n_taken=None, stream=None):
     """powattn_page_tables.  q_start, q_len int32 [b]; free_pages int32 [n_free]; block_table int32 [b, table_stride], updated
     in place.  Returns (slots int32 [b, q_rows], kv_len int32 [b], n_taken int32 [1])."""
+    if _native is not None and stream is None:
+        r = _native.page_tables(pattern._values, q_start, q_len, free_pages, block_table, n_pages, q_rows, slots, kv_len, n_taken)
+        if r is not NotImplemented:
+            return r
     batch = q_start.shape[0]
     _int32("q_start", q_start, (batch,))
     _int32("q_len", q_len, (batch,))
@@ -676,6 +681,10 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, q_start=None, q_len=None, e
     """powattn_qk_norm_rope.  q: [b,Hq,N,D], k: [b,Hkv,N,D], any strides with contiguous components (views of the projections'
     output); weights [D]; inv_freq float32 [rot_dim / 2] or None (norm only); q_start, q_len int32 [b] or None.  Returns
     contiguous (q_out, k_out); rows at or beyond a sequence's q_len are left as they were (zeros in outputs made here)."""
+    if _native is not None and stream is None:
+        r = _native.qk_norm_rope(q, k, q_weight, k_weight, inv_freq, q_start, q_len, eps, interleaved, q_out, k_out)
+        if r is not NotImplemented:
+            return r
     strides, (batch, hq, hkv, rows, d), rot = _rope_arguments(q, k, q_weight, k_weight, inv_freq, q_start, q_len)
     new = torch.empty if q_len is None else torch.zeros
     if q_out is None:
@@ -709,6 +718,11 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, inv_freq, dq_out, dk_out, q_
     """powattn_qk_norm_rope_backward: the inputs of qk_norm_rope and the gradients of its outputs (contiguous).  dq, dk may have
     strides of their own (views of the gradient of the projections' output).  Returns (dq, dk, dq_weight, dk_weight), the last
     two float32 [D]; rows at or beyond a sequence's q_len are left as they were (zeros in gradients made here)."""
+    if _native is not None and stream is None:
+        r = _native.qk_norm_rope_backward(q, k, q_weight, k_weight, inv_freq, q_start, q_len, eps, interleaved, dq_out, dk_out, dq, dk,
+                                          dq_weight, dk_weight, workspace)
+        if r is not NotImplemented:
+            return r
     strides, (batch, hq, hkv, rows, d), rot = _rope_arguments(q, k, q_weight, k_weight, inv_freq, q_start, q_len)
     _output("dq_out", dq_out, (batch, hq, rows, d), q.dtype)
     _output("dk_out", dk_out, (batch, hkv, rows, d), q.dtype)
@@ -770,6 +784,8 @@ def _cache_q4(pattern, cache, hkv, d):
 def cache_store_q4(pattern: Pattern, k, v, cache, slots, stream=None):
     """powattn_cache_store_q4.  k, v: bf16 [b,Hkv,N,D], any strides with contiguous components; slots int32 [b, N], as
     page_tables gives them."""
+    if _native is not None and stream is None and _native.cache_store_q4(pattern._values, k, v, cache, slots) is None:
+        return
     strides = _rows("k", k), _rows("v", v)
     batch, hkv, rows, d = k.shape
     if v.shape != k.shape or v.dtype != k.dtype:
@@ -786,6 +802,10 @@ def cache_load_q4(pattern: Pattern, cache, block_table, rows: int, start=None, l
     """powattn_cache_load_q4.  block_table int32 [b, table_stride]; start, length int32 [b] or None (zeros; all rows).
     Returns (k, v), bf16 [b,Hkv,rows,D]: row r of sequence b is position start[b] + r; rows at or beyond length[b] are left as
     they were (zeros in tensors made here)."""
+    if _native is not None and stream is None:
+        r = _native.cache_load_q4(pattern._values, cache, block_table, rows, start, length, k, v)
+        if r is not NotImplemented:
+            return r
     if block_table.dim() != 2:
         raise ValueError("block_table must be int32 [batch, table_stride]")
     batch, hkv, d = block_table.shape[0], cache[0].shape[1], 2 * cache[0].shape[3]
@@ -824,6 +844,10 @@ def decode_paged_q4(pattern: Pattern, q, cache, block_table, kv_len, o=None, lse
                     want_lse=True, stream=None):
     """powattn_decode_paged_q4.  q/o: [b,Hq,D]; cache: a CacheQ4; block_table int32 [b, table_stride]; kv_len int32 [b]
     (0: nothing is attended, o is zeros and lse -inf).  Returns (o, lse)."""
+    if _native is not None and stream is None:
+        r = _native.decode_paged_q4(pattern._values, q, cache, block_table, kv_len, o, lse, softmax_scale, workspace, want_lse)
+        if r is not NotImplemented:
+            return r
     if q.dim() != 3 or not q.is_contiguous():
         raise ValueError("q must be contiguous [batch, heads, head_dim]")
     batch, hq, d = q.shape
