@@ -1,7 +1,10 @@
 // Rows of keys and values into the 4-bit cache and out of it (format: q4.h).
 //
-// Both move bytes and nothing else: a lane has 8 components, 16 bytes in bf16 and 4 in the cache, four lanes share a scale,
-// and a wavefront takes consecutive tokens of one head, so that its pieces of a page are one contiguous stretch.
+// Both move bytes and nothing else.  A lane has 8 components, 16 bytes in bf16 and 4 in the cache, four lanes share a scale.
+// Where there are rows enough, a lane has four consecutive ones: they mostly lie side by side in a page, and their scales
+// are one word then.  A workgroup looks its rows' slots (pages) up once and walks through heads, keys and values
+// together; the next head's rows are requested before the current one's are converted.  With few rows a lane has one, of the keys or
+// of the values.
 #include "common.h"
 #include "q4.h"
 
@@ -17,7 +20,7 @@ struct store_params {
   q4_rows in[2];                          // keys, values
   uint8_t* pages[2]; uint8_t* scales[2];
   const int32_t* slots;
-  int32_t n_tokens, rows, hkv, B, n_slots;
+  int32_t n_tokens, rows, hkv, B, n_slots, per_chunk;
 };
 
 template <bool VEC>
@@ -28,52 +31,87 @@ __device__ __forceinline__ u32x4 q4_load8(const uint16_t* p) {
   for (int i = 0; i < 4; ++i) r[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
   return r;
 }
+// Four consecutive rows whose slots (positions) follow one another from a multiple of four on, which four rows of a page do
+template <int TOK>
+__device__ __forceinline__ bool q4_side_by_side(const int32_t (&slot)[TOK]) {
+  if constexpr (TOK != 4) return false;
+  else return slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3;
+}
 
-// D: head_dim; TOK: tokens of a lane, a wavefront's worth apart, all of them requested before any is used
+// D: head_dim; TOK: consecutive rows of a lane, of keys and of values (one: blockIdx.z says of which)
 template <int D, int TOK, bool VEC>
 __global__ __launch_bounds__(THREADS) void pa_cache_store_q4_kernel(store_params p) {
-  constexpr int LPR = D / 8, STEP = THREADS / LPR;          // lanes of a row, rows side by side
-  const int lane = threadIdx.x % LPR, kv = blockIdx.z, h = blockIdx.y;
-  const int t0 = blockIdx.x * (STEP * TOK) + threadIdx.x / LPR;
-  const q4_rows in = p.in[kv];
+  constexpr int LPR = D / 8, NKV = TOK == 1 ? 1 : 2;        // lanes of a row
+  const int lane = threadIdx.x % LPR, kv0 = NKV == 1 ? blockIdx.z : 0;
+  const int64_t t0 = ((int64_t)blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR) * TOK;
+  const int h0 = blockIdx.y * p.per_chunk, h1 = min(h0 + p.per_chunk, p.hkv);
   int32_t slot[TOK];
-  u32x4 x[TOK];
+  const uint16_t* from[NKV][TOK];
+  int64_t page[TOK]; int32_t off[TOK];
+  bool any = false;
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    const int t = t0 + i * STEP;
-    slot[i] = t < p.n_tokens ? p.slots[t] : -1;
+    slot[i] = t0 + i < p.n_tokens ? p.slots[t0 + i] : -1;
+    if (slot[i] >= p.n_slots) slot[i] = -1;                 // rows without a slot are not read
+    any = any || slot[i] >= 0;
   }
+  if (!any) return;                                         // (the lanes of a row stay together)
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    x[i] = u32x4{0, 0, 0, 0};
-    if (slot[i] < 0 || slot[i] >= p.n_slots) continue;      // rows without a slot are not read
-    const unsigned t = t0 + i * STEP, b = t / (unsigned)p.rows, r = t - b * (unsigned)p.rows;
-    x[i] = q4_load8<VEC>(in.p + b * in.sb + h * in.sh + r * in.sr + 8 * lane);
+    const unsigned t = (unsigned)(t0 + i), b = t / (unsigned)p.rows, r = t - b * (unsigned)p.rows;
+#pragma unroll
+    for (int kv = 0; kv < NKV; ++kv) from[kv][i] = p.in[kv0 + kv].p + b * p.in[kv0 + kv].sb + r * p.in[kv0 + kv].sr + 8 * lane;
+    const unsigned pg = (unsigned)max(slot[i], 0) / (unsigned)p.B;
+    page[i] = (int64_t)pg * p.hkv;
+    off[i] = max(slot[i], 0) - (int)pg * p.B;
   }
+  const bool together = q4_side_by_side<TOK>(slot);         // (a block is a multiple of 64 rows: they are in one page)
+  u32x4 x[NKV][TOK], next[NKV][TOK];
+  auto request = [&](u32x4 (&y)[NKV][TOK], int h) {
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    uint32_t amax = 0;
+    for (int kv = 0; kv < NKV; ++kv)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t lo = (x[i][e] & 0x7fffu) << 16, hi = x[i][e] & 0x7fff0000u;      // magnitudes order like their bits
-      amax = max(amax, max(lo, hi));
+      for (int i = 0; i < TOK; ++i) {
+        y[kv][i] = u32x4{0, 0, 0, 0};
+        if (slot[i] >= 0) y[kv][i] = q4_load8<VEC>(from[kv][i] + h * p.in[kv0 + kv].sh);
+      }
+  };
+  request(x, h0);
+  for (int h = h0; h < h1; ++h) {
+    if (h + 1 < h1) request(next, h + 1);
+#pragma unroll
+    for (int kv = 0; kv < NKV; ++kv) {
+      uint32_t codes = 0;
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) {
+        const u32x4 y = x[kv][i];
+        uint32_t amax = 0;                                  // magnitudes order like their bits
+#pragma unroll
+        for (int e = 0; e < 4; ++e) amax = max(amax, max((y[e] & 0x7fffu) << 16, y[e] & 0x7fff0000u));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+        const uint32_t code = q4_scale_code(amax);
+        uint32_t word = 0;
+        if (code != 255u) {
+          const float scale = q4_scale(code);
+          word = q4_shrink<0>(word, y[0], scale);
+          word = q4_shrink<1>(word, y[1], scale);
+          word = q4_shrink<2>(word, y[2], scale);
+          word = q4_shrink<3>(word, y[3], scale);
+        }
+        codes |= code << (8 * i);
+        if (slot[i] < 0) continue;
+        const int64_t at = page[i] + h;
+        *reinterpret_cast<uint32_t*>(p.pages[kv0 + kv] + (at * p.B + off[i]) * (D / 2) + 4 * lane) = word;
+        if ((lane & 3) == 0 && !together) p.scales[kv0 + kv][(at * (D / 32) + (lane >> 2)) * p.B + off[i]] = (uint8_t)code;
+      }
+      if ((lane & 3) == 0 && together)
+        *reinterpret_cast<uint32_t*>(p.scales[kv0 + kv] + ((page[0] + h) * (D / 32) + (lane >> 2)) * p.B + off[0]) = codes;
     }
-    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
-    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
-    if (slot[i] < 0 || slot[i] >= p.n_slots) continue;
-    const uint32_t code = q4_scale_code(amax);
-    uint32_t word = 0;
-    if (code != 255u) {
-      const float scale = q4_scale(code);
-      word = q4_shrink<0>(word, x[i][0], scale);
-      word = q4_shrink<1>(word, x[i][1], scale);
-      word = q4_shrink<2>(word, x[i][2], scale);
-      word = q4_shrink<3>(word, x[i][3], scale);
-    }
-    const unsigned page = (unsigned)slot[i] / (unsigned)p.B, off = (unsigned)slot[i] - page * (unsigned)p.B;
-    const int64_t at = (int64_t)page * p.hkv + h;
-    *reinterpret_cast<uint32_t*>(p.pages[kv] + (at * p.B + off) * (D / 2) + 4 * lane) = word;
-    if ((lane & 3) == 0) p.scales[kv][(at * (D / 32) + (lane >> 2)) * p.B + off] = (uint8_t)code;
+#pragma unroll
+    for (int kv = 0; kv < NKV; ++kv)
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) x[kv][i] = next[kv][i];
   }
 }
 
@@ -81,41 +119,72 @@ struct load_params {
   const uint8_t* pages[2]; const uint8_t* scales[2];
   uint16_t* out[2];                       // [batch, heads, rows, head_dim]
   const int32_t* table; const int32_t* start; const int32_t* length;
-  int32_t n_tokens, rows, hkv, B, stride, last_page, capacity;
+  int32_t n_tokens, rows, hkv, B, stride, last_page, capacity, per_chunk;
 };
 
 template <int D, int TOK>
 __global__ __launch_bounds__(THREADS) void pa_cache_load_q4_kernel(load_params p) {
-  constexpr int LPR = D / 8, STEP = THREADS / LPR;
-  const int lane = threadIdx.x % LPR, kv = blockIdx.z, h = blockIdx.y;
-  const int t0 = blockIdx.x * (STEP * TOK) + threadIdx.x / LPR;
-  uint32_t word[TOK], code[TOK];
-  int64_t to[TOK];
+  constexpr int LPR = D / 8, NKV = TOK == 1 ? 1 : 2;
+  const int lane = threadIdx.x % LPR, kv0 = NKV == 1 ? blockIdx.z : 0;
+  const int64_t t0 = ((int64_t)blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR) * TOK;
+  const int h0 = blockIdx.y * p.per_chunk, h1 = min(h0 + p.per_chunk, p.hkv);
+  int64_t page[TOK], to[TOK];
+  int32_t off[TOK], where[TOK];
+  bool any = false;
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    const unsigned t = t0 + i * STEP;
-    to[i] = -1;
-    word[i] = code[i] = 0;
-    if (t >= (unsigned)p.n_tokens) continue;
-    const unsigned b = t / (unsigned)p.rows, r = t - b * (unsigned)p.rows;
+    where[i] = -1;
+    page[i] = to[i] = off[i] = 0;
+    if (t0 + i >= p.n_tokens) continue;
+    const unsigned t = (unsigned)(t0 + i), b = t / (unsigned)p.rows, r = t - b * (unsigned)p.rows;
     int32_t s = p.start ? p.start[b] : 0, n = p.length ? p.length[b] : p.rows;
     s = s < 0 ? 0 : (s > p.capacity ? p.capacity : s);
     if (n > p.capacity - s) n = p.capacity - s;
     if ((int32_t)r >= n) continue;
-    const unsigned pos = (unsigned)s + r, blk = pos / (unsigned)p.B, off = pos - blk * (unsigned)p.B;
-    int page = p.table[(int64_t)b * p.stride + blk];
-    page = page < 0 ? 0 : (page > p.last_page ? p.last_page : page);     // a bad table gives wrong numbers, no stray access
-    const int64_t at = (int64_t)page * p.hkv + h;
-    word[i] = *reinterpret_cast<const uint32_t*>(p.pages[kv] + (at * p.B + off) * (D / 2) + 4 * lane);
-    code[i] = p.scales[kv][(at * (D / 32) + (lane >> 2)) * p.B + off];
-    to[i] = (((int64_t)b * p.hkv + h) * p.rows + r) * D + 8 * lane;
+    const unsigned pos = (unsigned)s + r, blk = pos / (unsigned)p.B;
+    int pg = p.table[(int64_t)b * p.stride + blk];
+    pg = pg < 0 ? 0 : (pg > p.last_page ? p.last_page : pg);             // a bad table gives wrong numbers, no stray access
+    page[i] = (int64_t)pg * p.hkv;
+    off[i] = (int32_t)(pos - blk * (unsigned)p.B);
+    where[i] = pg * p.B + off[i];
+    to[i] = ((int64_t)b * p.hkv * p.rows + r) * D + 8 * lane;
+    any = true;
   }
+  if (!any) return;
+  const bool together = q4_side_by_side<TOK>(where);
+  uint32_t word[NKV][TOK], code[NKV][TOK], next_word[NKV][TOK], next_code[NKV][TOK];
+  auto request = [&](uint32_t (&w)[NKV][TOK], uint32_t (&c)[NKV][TOK], int h) {
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    if (to[i] < 0) continue;
-    const float scale = q4_scale(code[i]);
-    const u32x4 x = {q4_expand<0>(word[i], scale), q4_expand<1>(word[i], scale), q4_expand<2>(word[i], scale), q4_expand<3>(word[i], scale)};
-    *reinterpret_cast<u32x4*>(p.out[kv] + to[i]) = x;
+    for (int kv = 0; kv < NKV; ++kv) {
+      if (together) c[kv][0] = *reinterpret_cast<const uint32_t*>(p.scales[kv0 + kv] + ((page[0] + h) * (D / 32) + (lane >> 2)) * p.B + off[0]);
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) {
+        if (where[i] < 0) continue;
+        const int64_t at = page[i] + h;
+        w[kv][i] = *reinterpret_cast<const uint32_t*>(p.pages[kv0 + kv] + (at * p.B + off[i]) * (D / 2) + 4 * lane);
+        if (!together) c[kv][i] = p.scales[kv0 + kv][(at * (D / 32) + (lane >> 2)) * p.B + off[i]];
+      }
+    }
+  };
+  request(word, code, h0);
+  for (int h = h0; h < h1; ++h) {
+    if (h + 1 < h1) request(next_word, next_code, h + 1);
+#pragma unroll
+    for (int kv = 0; kv < NKV; ++kv)
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) {
+        if (where[i] < 0) continue;
+        const float scale = q4_scale(together ? code[kv][0] >> (8 * i) & 255u : code[kv][i]);
+        const uint32_t w = word[kv][i];
+        const u32x4 x = {q4_expand<0>(w, scale), q4_expand<1>(w, scale), q4_expand<2>(w, scale), q4_expand<3>(w, scale)};
+        u32x4* to_row = reinterpret_cast<u32x4*>(p.out[kv0 + kv] + to[i] + (int64_t)h * p.rows * D);
+        if constexpr (TOK == 4) __builtin_nontemporal_store(x, to_row);      // (us, 32 pieces of up to 2048 rows: 45 -> 40)
+        else *to_row = x;
+      }
+#pragma unroll
+    for (int kv = 0; kv < NKV; ++kv)
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) { word[kv][i] = next_word[kv][i]; code[kv][i] = next_code[kv][i]; }
   }
 }
 
@@ -130,11 +199,20 @@ int check_cache(const powattn_pattern* pattern, int32_t batch, int32_t hkv, int6
   return POWATTN_OK;
 }
 
-// Tokens of a lane: four where that leaves eight wavefronts for every compute unit, else one.
-int tokens_of_a_lane(int64_t n_tokens, int32_t hkv, int32_t head_dim) {
+// The launch: four rows of a lane where that leaves a workgroup for every compute unit, else one; as many heads of a workgroup as
+// leave eight workgroups for every compute unit.
+struct q4_launch { int tok; int32_t per_chunk; dim3 grid; };
+bool launch_of(q4_launch& l, int64_t n_tokens, int32_t hkv, int32_t head_dim) {
   int n_cu = 1;
   pa_current_device(nullptr, &n_cu);
-  return n_tokens * hkv * 2 * (head_dim / 8) >= (int64_t)n_cu * 4 * 8 * 64 ? 4 : 1;
+  const int64_t side = THREADS / (head_dim / 8);
+  l.tok = n_tokens * hkv >= 4 * side * n_cu ? 4 : 1;
+  const int64_t groups = (n_tokens + side * l.tok - 1) / (side * l.tok);
+  int64_t chunks = (8 * (int64_t)n_cu + groups - 1) / groups;
+  if (chunks > hkv) chunks = hkv;
+  l.per_chunk = (int32_t)((hkv + chunks - 1) / chunks);
+  l.grid = dim3((uint32_t)groups, (uint32_t)((hkv + l.per_chunk - 1) / l.per_chunk), l.tok == 1 ? 2 : 1);
+  return (int64_t)l.grid.x * l.grid.y * l.grid.z <= 0xffffffffLL / THREADS;      // a launch has fewer than 2^32 threads
 }
 
 }  // namespace
@@ -147,7 +225,7 @@ extern "C" int powattn_cache_store_q4(const powattn_pattern* pattern, const void
   if (st != POWATTN_OK) return st;
   if (!k || !v || !k_strides || !v_strides || !d_slots || !k_pages || !v_pages || !k_scales || !v_scales) return POWATTN_INVALID_ARG;
   if ((st = check_cache(pattern, batch, n_kv_heads, rows, n_pages, head_dim, dtype)) != POWATTN_OK) return st;
-  if (((uintptr_t)k_pages | (uintptr_t)v_pages) & 15u) return POWATTN_INVALID_ARG;
+  if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)k_scales | (uintptr_t)v_scales) & 15u) return POWATTN_INVALID_ARG;
   if (((uintptr_t)k | (uintptr_t)v) & 1u) return POWATTN_INVALID_ARG;
   store_params p;
   p.in[0] = {(const uint16_t*)k, k_strides[0], k_strides[1], k_strides[2]};
@@ -159,16 +237,16 @@ extern "C" int powattn_cache_store_q4(const powattn_pattern* pattern, const void
   p.n_slots = (int32_t)(n_pages * pattern->block);
   bool vec = (((uintptr_t)k | (uintptr_t)v) & 15u) == 0;
   for (int i = 0; i < 3; ++i) vec = vec && k_strides[i] % 8 == 0 && v_strides[i] % 8 == 0;
-  const int tok = tokens_of_a_lane(p.n_tokens, n_kv_heads, head_dim), step = THREADS / (head_dim / 8);
-  const dim3 grid((uint32_t)((p.n_tokens + (int64_t)step * tok - 1) / ((int64_t)step * tok)), (uint32_t)n_kv_heads, 2);
-  if ((int64_t)grid.x * grid.y * 2 > 0xffffffffLL / THREADS) return POWATTN_UNSUPPORTED;   // a launch has fewer than 2^32 threads
+  q4_launch l;
+  if (!launch_of(l, p.n_tokens, n_kv_heads, head_dim)) return POWATTN_UNSUPPORTED;
+  p.per_chunk = l.per_chunk;
   hipStream_t stream = (hipStream_t)hip_stream;
-#define STORE(D, TOK, VEC) hipLaunchKernelGGL((pa_cache_store_q4_kernel<D, TOK, VEC>), grid, dim3(THREADS), 0, stream, p)
+#define STORE(D, TOK, VEC) hipLaunchKernelGGL((pa_cache_store_q4_kernel<D, TOK, VEC>), l.grid, dim3(THREADS), 0, stream, p)
   if (head_dim == 128) {
-    if (tok == 4) { if (vec) STORE(128, 4, true); else STORE(128, 4, false); }
+    if (l.tok == 4) { if (vec) STORE(128, 4, true); else STORE(128, 4, false); }
     else { if (vec) STORE(128, 1, true); else STORE(128, 1, false); }
   } else {
-    if (tok == 4) { if (vec) STORE(64, 4, true); else STORE(64, 4, false); }
+    if (l.tok == 4) { if (vec) STORE(64, 4, true); else STORE(64, 4, false); }
     else { if (vec) STORE(64, 1, true); else STORE(64, 1, false); }
   }
 #undef STORE
@@ -184,7 +262,7 @@ extern "C" int powattn_cache_load_q4(const powattn_pattern* pattern, const void*
   if (!k || !v || !d_block_table || !k_pages || !v_pages || !k_scales || !v_scales) return POWATTN_INVALID_ARG;
   if (table_stride < 1) return POWATTN_INVALID_ARG;
   if ((st = check_cache(pattern, batch, n_kv_heads, rows, n_pages, head_dim, dtype)) != POWATTN_OK) return st;
-  if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)k | (uintptr_t)v) & 15u) return POWATTN_INVALID_ARG;
+  if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)k_scales | (uintptr_t)v_scales | (uintptr_t)k | (uintptr_t)v) & 15u) return POWATTN_INVALID_ARG;
   const int64_t capacity = (int64_t)table_stride * pattern->block;
   if (capacity > 0x7fffffff) return POWATTN_UNSUPPORTED;
   load_params p;
@@ -194,13 +272,13 @@ extern "C" int powattn_cache_load_q4(const powattn_pattern* pattern, const void*
   p.table = d_block_table; p.start = d_start; p.length = d_length;
   p.n_tokens = (int32_t)(batch * rows); p.rows = (int32_t)rows; p.hkv = n_kv_heads; p.B = pattern->block;
   p.stride = table_stride; p.last_page = (int32_t)n_pages - 1; p.capacity = (int32_t)capacity;
-  const int tok = tokens_of_a_lane(p.n_tokens, n_kv_heads, head_dim), step = THREADS / (head_dim / 8);
-  const dim3 grid((uint32_t)((p.n_tokens + (int64_t)step * tok - 1) / ((int64_t)step * tok)), (uint32_t)n_kv_heads, 2);
-  if ((int64_t)grid.x * grid.y * 2 > 0xffffffffLL / THREADS) return POWATTN_UNSUPPORTED;
+  q4_launch l;
+  if (!launch_of(l, p.n_tokens, n_kv_heads, head_dim)) return POWATTN_UNSUPPORTED;
+  p.per_chunk = l.per_chunk;
   hipStream_t stream = (hipStream_t)hip_stream;
-#define LOAD(D, TOK) hipLaunchKernelGGL((pa_cache_load_q4_kernel<D, TOK>), grid, dim3(THREADS), 0, stream, p)
-  if (head_dim == 128) { if (tok == 4) LOAD(128, 4); else LOAD(128, 1); }
-  else { if (tok == 4) LOAD(64, 4); else LOAD(64, 1); }
+#define LOAD(D, TOK) hipLaunchKernelGGL((pa_cache_load_q4_kernel<D, TOK>), l.grid, dim3(THREADS), 0, stream, p)
+  if (head_dim == 128) { if (l.tok == 4) LOAD(128, 4); else LOAD(128, 1); }
+  else { if (l.tok == 4) LOAD(64, 4); else LOAD(64, 1); }
 #undef LOAD
   return pa_note_hip(hipGetLastError());
 }

@@ -94,7 +94,8 @@ def test_cache_q4_argument_errors(L, call):
         assert call(L, **{name: None}) == pa.INVALID_ARG, name
     for name in ("batch", "hkv", "rows", "d", "n_pages") + (() if call is _store else ("stride",)):
         assert call(L, **{name: 0}) == pa.INVALID_ARG, name
-    assert call(L, kp=FAKE + 8) == pa.INVALID_ARG
+    for name in ("kp", "vp", "ksc", "vsc"):
+        assert call(L, **{name: FAKE + 8}) == pa.INVALID_ARG, name
     assert call(L, pat=pa.Pattern(64, -1, 1)) == pa.INVALID_ARG
     assert call(L, pat=pa.Pattern(48, 4, 1)) == pa.UNSUPPORTED
     assert call(L, pat=pa.Pattern(2048, 4, 1)) == pa.UNSUPPORTED
