@@ -15,7 +15,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int THREADS = 256;
-constexpr int AHEAD = 4;                 // heads whose rows are requested together
+constexpr int AHEAD = 2;                 // heads whose rows are requested together, while those before them are in use
 
 // rows [batch, heads, rows, head_dim], strides in elements
 struct nr_rows { const void* p; int64_t sb, sh, sr; };
@@ -72,24 +72,30 @@ __device__ __forceinline__ void nr_floats(float (&f)[8], const raw8<float>& r) {
     f[4 + i] = __builtin_bit_cast(float, b);
   }
 }
-template <bool VEC>
+// MODE 0: components one at a time, 1: 16 bytes at a time, 2: the same past the caches
+template <int MODE>
+__device__ __forceinline__ void nr_put16(void* p, u32x4 x) {
+  if constexpr (MODE == 2) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
+  else *reinterpret_cast<u32x4*>(p) = x;
+}
+template <int MODE>
 __device__ __forceinline__ void nr_store(__bf16* p, const float (&f)[8]) {
   typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
   bf16x8 y;
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = (__bf16)f[i];
-  if constexpr (VEC) *reinterpret_cast<bf16x8*>(p) = y;
+  if constexpr (MODE > 0) nr_put16<MODE>(p, __builtin_bit_cast(u32x4, y));
   else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = y[i];
   }
 }
-template <bool VEC>
+template <int MODE>
 __device__ __forceinline__ void nr_store(float* p, const float (&f)[8]) {
   typedef float f32x4 __attribute__((ext_vector_type(4)));
-  if constexpr (VEC) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{f[0], f[1], f[2], f[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{f[4], f[5], f[6], f[7]};
+  if constexpr (MODE > 0) {
+    nr_put16<MODE>(p, __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}));
+    nr_put16<MODE>(p + 4, __builtin_bit_cast(u32x4, f32x4{f[4], f[5], f[6], f[7]}));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = f[i];
@@ -149,9 +155,10 @@ __device__ __forceinline__ float nr_sum(float x) {
   return x;
 }
 
-template <class T, int D, bool VEC, bool INTER>
+template <class T, int D, int MODE, bool INTER>
 __global__ __launch_bounds__(THREADS) void pa_qk_norm_rope_kernel(nr_params p) {
   constexpr int LPR = D / 16;
+  constexpr bool VEC = MODE > 0;
   const int c = threadIdx.x % LPR;
   const int t = blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR;
   int chunk = blockIdx.y;
@@ -172,19 +179,23 @@ __global__ __launch_bounds__(THREADS) void pa_qk_norm_rope_kernel(nr_params p) {
   const T* x = (const T*)p.x[which].p + b * p.x[which].sb + r * p.x[which].sr;
   T* y = (T*)p.out[which].p + b * p.out[which].sb + r * p.out[which].sr;
   const int64_t xh = p.x[which].sh, yh = p.out[which].sh;
+  raw8<T> ra[AHEAD], rb[AHEAD], na[AHEAD], nb[AHEAD];
+  auto request = [&](raw8<T> (&u)[AHEAD], raw8<T> (&v)[AHEAD], int h) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (h + i >= h1) break;
+      nr_load<VEC>(u[i], x + (h + i) * xh + at.a);
+      nr_load<VEC>(v[i], x + (h + i) * xh + at.b);
+    }
+  };
+  request(ra, rb, h0);                     // (under way while the angles are formed)
   nr_angles(cs, sn, turns, (int64_t)(p.q_start ? p.q_start[b] : 0) + r);
   float w0[8], w1[8];
   nr_floats(w0, wa);
   nr_floats(w1, wb);
 
   for (int h = h0; h < h1; h += AHEAD) {
-    raw8<T> ra[AHEAD], rb[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      if (h + i >= h1) break;
-      nr_load<VEC>(ra[i], x + (h + i) * xh + at.a);
-      nr_load<VEC>(rb[i], x + (h + i) * xh + at.b);
-    }
+    request(na, nb, h + AHEAD);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (h + i >= h1) break;
@@ -197,17 +208,21 @@ __global__ __launch_bounds__(THREADS) void pa_qk_norm_rope_kernel(nr_params p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) { f0[e] = f0[e] * rn * w0[e]; f1[e] = f1[e] * rn * w1[e]; }
       if (at.turned) nr_rotate<INTER>(f0, f1, cs, sn);
-      nr_store<VEC>(y + (h + i) * yh + at.a, f0);
-      nr_store<VEC>(y + (h + i) * yh + at.b, f1);
+      nr_store<MODE>(y + (h + i) * yh + at.a, f0);
+      nr_store<MODE>(y + (h + i) * yh + at.b, f1);
     }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) { ra[i] = na[i]; rb[i] = nb[i]; }
   }
 }
 
 // Gradients: a workgroup walks through every gridDim.x-th group of tokens with its heads, keeps its sums of dw in registers
-// and leaves them in the workspace; the sums of all workgroups are added by the kernel below, in a fixed order.
-template <class T, int D, bool VEC, bool INTER>
+// and leaves them in the workspace; the sums of all workgroups are added by the kernel below, in a fixed order.  (The next
+// head's rows requested ahead, as above, cost a third of the wavefronts: 32768 rows 175 -> 169 us, 1000 13.5 -> 16.9, 8192 61.7 -> 64.3.)
+template <class T, int D, int MODE, bool INTER>
 __global__ __launch_bounds__(THREADS) void pa_qk_norm_rope_grad_kernel(nr_params p) {
   constexpr int LPR = D / 16, TOK = THREADS / LPR, NWV = THREADS / 64;
+  constexpr bool VEC = MODE > 0;
   __shared__ float s_dw[NWV][D];
   const int c = threadIdx.x % LPR;
   int chunk = blockIdx.y;
@@ -264,8 +279,8 @@ __global__ __launch_bounds__(THREADS) void pa_qk_norm_rope_grad_kernel(nr_params
         d0[e] = rn * (d0[e] * w0[e] - k * f0[e]);
         d1[e] = rn * (d1[e] * w1[e] - k * f1[e]);
       }
-      nr_store<VEC>(o + h * oh + at.a, d0);
-      nr_store<VEC>(o + h * oh + at.b, d1);
+      nr_store<MODE>(o + h * oh + at.a, d0);
+      nr_store<MODE>(o + h * oh + at.b, d1);
     }
   }
 
@@ -296,15 +311,21 @@ __global__ __launch_bounds__(SUM_THREADS) void pa_qk_norm_rope_sum_kernel(const 
   const float* part = blockIdx.y ? part_k : part_q;
   const int n = blockIdx.y ? n_k : n_q;
   const int col = threadIdx.x % SUM_COLS, row = threadIdx.x / SUM_COLS, d = blockIdx.x * SUM_COLS + col;
+  constexpr int ROWS = SUM_THREADS / SUM_COLS, AT_ONCE = 16;
   float a = 0.f;
-#pragma unroll 4
-  for (int i = row; i < n; i += SUM_THREADS / SUM_COLS) a += part[(int64_t)i * D + d];
+  for (int i0 = row; i0 < n; i0 += ROWS * AT_ONCE) {       // a trip to memory for 16 rows
+    float x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) x[j] = i0 + j * ROWS < n ? part[(int64_t)(i0 + j * ROWS) * D + d] : 0.f;
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) a += x[j];
+  }
   s[row][col] = a;
   __syncthreads();
   if (row == 0) {
     float all = 0.f;
 #pragma unroll
-    for (int i = 0; i < SUM_THREADS / SUM_COLS; ++i) all += s[i][col];
+    for (int i = 0; i < ROWS; ++i) all += s[i][col];
     (blockIdx.y ? dw_k : dw_q)[d] = all;
   }
 }
@@ -340,7 +361,7 @@ nr_grid grad_grid(nr_params& p, int32_t head_dim) {
   const int64_t tok = THREADS / (head_dim / 16);
   nr_grid g;
   g.groups = (p.n_tokens + tok - 1) / tok;
-  deal_heads(p, g.groups, 1024);
+  deal_heads(p, g.groups, 1024);                           // (us, 2048 / 8192 rows of 40 heads, 1024 workgroups 21.6 / 61.2, 640 18.0 / 66.7)
   const int64_t chunks = p.chunks[0] + p.chunks[1];
   int64_t x = (2048 + chunks - 1) / chunks;
   if (x > g.groups) x = g.groups;
@@ -363,28 +384,33 @@ int check_rotation(int32_t rot, int32_t head_dim, uint32_t flags, float eps) {
   return POWATTN_OK;
 }
 
-template <class T, int D, bool VEC>
+template <class T, int D, int MODE>
 void launch_forward(const nr_params& p, dim3 grid, bool inter, hipStream_t s) {
-  if (inter) hipLaunchKernelGGL((pa_qk_norm_rope_kernel<T, D, VEC, true>), grid, dim3(THREADS), 0, s, p);
-  else hipLaunchKernelGGL((pa_qk_norm_rope_kernel<T, D, VEC, false>), grid, dim3(THREADS), 0, s, p);
+  if (inter) hipLaunchKernelGGL((pa_qk_norm_rope_kernel<T, D, MODE, true>), grid, dim3(THREADS), 0, s, p);
+  else hipLaunchKernelGGL((pa_qk_norm_rope_kernel<T, D, MODE, false>), grid, dim3(THREADS), 0, s, p);
 }
-template <class T, int D, bool VEC>
+template <class T, int D, int MODE>
 void launch_grad(const nr_params& p, dim3 grid, bool inter, hipStream_t s) {
-  if (inter) hipLaunchKernelGGL((pa_qk_norm_rope_grad_kernel<T, D, VEC, true>), grid, dim3(THREADS), 0, s, p);
-  else hipLaunchKernelGGL((pa_qk_norm_rope_grad_kernel<T, D, VEC, false>), grid, dim3(THREADS), 0, s, p);
+  if (inter) hipLaunchKernelGGL((pa_qk_norm_rope_grad_kernel<T, D, MODE, true>), grid, dim3(THREADS), 0, s, p);
+  else hipLaunchKernelGGL((pa_qk_norm_rope_grad_kernel<T, D, MODE, false>), grid, dim3(THREADS), 0, s, p);
 }
 template <bool GRAD, class T>
-void launch_d(const nr_params& p, dim3 grid, int32_t head_dim, bool vec, bool inter, hipStream_t s) {
-#define GO(D, VEC) do { if constexpr (GRAD) launch_grad<T, D, VEC>(p, grid, inter, s); else launch_forward<T, D, VEC>(p, grid, inter, s); } while (0)
-  if (head_dim == 128) { if (vec) GO(128, true); else GO(128, false); }
-  else { if (vec) GO(64, true); else GO(64, false); }
+void launch_d(const nr_params& p, dim3 grid, int32_t head_dim, int mode, bool inter, hipStream_t s) {
+#define GO(D, MODE) do { if constexpr (GRAD) launch_grad<T, D, MODE>(p, grid, inter, s); else launch_forward<T, D, MODE>(p, grid, inter, s); } while (0)
+  if (head_dim == 128) { if (mode == 2) GO(128, 2); else if (mode == 1) GO(128, 1); else GO(128, 0); }
+  else { if (mode == 2) GO(64, 2); else if (mode == 1) GO(64, 1); else GO(64, 0); }
 #undef GO
 }
+// The outputs go past the caches where the tensors together are larger than half of the 256 MB behind the L2s: what is written
+// would push out what is still to be read.  us, through / past, 40 heads of 128 in bf16: 32768 rows (537 MB, 32 heads) 109 / 105, 8192 (168 MB)
+// 41.6 / 29.7, their gradients 179 / 175 and 64.4 / 62.1; 8192 rows of 64 (84 MB) 17.0 / 19.9.
 template <bool GRAD>
 int launch(const nr_params& p, dim3 grid, int32_t head_dim, int32_t dtype, bool inter, hipStream_t s) {
-  const bool vec = aligned(p, GRAD, dtype == POWATTN_F32 ? 4 : 2);
-  if (dtype == POWATTN_F32) launch_d<GRAD, float>(p, grid, head_dim, vec, inter, s);
-  else launch_d<GRAD, __bf16>(p, grid, head_dim, vec, inter, s);
+  const int64_t elem = dtype == POWATTN_F32 ? 4 : 2;
+  const int64_t bytes = (GRAD ? 3 : 2) * elem * p.n_tokens * head_dim * (p.heads[0] + p.heads[1]);
+  const int mode = !aligned(p, GRAD, elem) ? 0 : bytes > (128 << 20) ? 2 : 1;
+  if (dtype == POWATTN_F32) launch_d<GRAD, float>(p, grid, head_dim, mode, inter, s);
+  else launch_d<GRAD, __bf16>(p, grid, head_dim, mode, inter, s);
   return pa_note_hip(hipGetLastError());
 }
 

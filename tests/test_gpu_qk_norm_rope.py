@@ -186,3 +186,22 @@ def test_rows_of_zeros_and_without_numbers():
     assert (out[0, 0, 2] == 0).all() and out[0, 1, 3].isnan().all()
     assert out[0, 1, 4, 100].isnan() and torch.isfinite(out[0, 1, 4, 64:100]).all()        # inf / inf; the others are 0
     assert torch.isfinite(out[0, 0]).all() and torch.isfinite(out[0, 1, [0, 1, 2, 5]]).all()
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 16384), ("f32", 9000)])
+def test_a_large_call_is_its_parts(dtype, n):
+    # beyond 128 MB the outputs are written past the caches: the same bits as from calls on parts of the rows
+    b, hq, hkv, d = 1, 18, 2, 128
+    q, k, w, inv = inputs(dtype, b, hq, hkv, n, d, d, 51)
+    gen = torch.Generator("cuda").manual_seed(52)
+    q, k, w, inv = on_gpu(q), on_gpu(k), [x.cuda() for x in w], inv.cuda()
+    dy = [torch.randn(x.shape, generator=gen, device="cuda").to(TYPES[dtype]) for x in (q, k)]
+    assert 2 * (q.numel() + k.numel()) * q.element_size() > 128 << 20
+    outs, grads = pa.qk_norm_rope(q, k, *w, inv), pa.qk_norm_rope_backward(q, k, *w, inv, *dy)
+    for lo, hi in ((0, 3000), (3000, 3001), (n - 2500, n)):
+        start = torch.tensor([lo], dtype=torch.int32, device="cuda")
+        parts = [x[:, :, lo:hi] for x in (q, k)]
+        got = pa.qk_norm_rope(*parts, *w, inv, q_start=start)
+        assert all(torch.equal(a[:, :, lo:hi], x) for a, x in zip(outs, got))
+        got = pa.qk_norm_rope_backward(*parts, *w, inv, *(x[:, :, lo:hi].contiguous() for x in dy), q_start=start)
+        assert all(torch.equal(a[:, :, lo:hi], x) for a, x in zip(grads[:2], got[:2]))
