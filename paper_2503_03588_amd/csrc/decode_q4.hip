@@ -1,19 +1,17 @@
 // Split-K decode over a paged cache held in 4 bits (format: q4.h): the step of decode.hip with pages of 4-bit keys and values.
 //
 // A step reads 2 * (head_dim / 2 + head_dim / 32) bytes per attended token and KV head, 0.27 of the bf16 step's, so that
-// it is bound by latency and by the instructions of expanding the cache rather than by memory.
+// it is bound by latency and by the instructions of expanding the cache (about 430 a chunk) rather than by memory,
+// until there are enough sequences.  Keys and values are expanded to bf16 in registers, exactly (a 4-bit value
+// times a power of two is a bf16 number), and multiplied with v_mfma_f32_16x16x32_bf16.
 //  * A chunk is 64 tokens of a block; a wavefront requests all of one before it uses any.  Token 4i + T of it is row i of tile T
-//    (T = 0..3) of S^T = K q^T, and lane (g, q4) (g = lane % 16, q4 = lane / 16) then has the scores of tokens
-//    16 q4 .. 16 q4 + 15.
-//  * Keys are not expanded: v_mfma_scale_f32_16x16x128_f8f6f4 takes 4-bit rows with their scales, which are the bytes of one
-//    word for a lane's rows of the four tiles.  The other operand is the query in 8 bits, as the sum of two e4m3 numbers with a power of two each
-//    for the row: of bf16's 8 bits each has 4 (sign and one implicit bit apart), so the sum is exact for components down to
-//    2^-13 of the row's largest, and off by at most 2^-22 of that below, which is less than the rounding of the
-//    sum in fp32.  (Expanding the keys to bf16 instead takes 64 conversions and 8 more products a chunk.)
-//  * Values are expanded to bf16, exactly.  The conversion yields two neighbouring components of a token; where the
-//    product wants pairs along the tokens, a token counts twice in its sum, once for each component, and P is held with zeros in
-//    the other place: O_even and O_odd are different columns.  (Bringing pairs of tokens together by byte permutes: 64 more
-//    instructions a chunk, and as many products.)
+//    (T = 0..3) of S^T = K q^T: a lane's piece of a K row lies in one scale's 32 components, the scales of its four tiles are
+//    the bytes of one word, and lane (g, q4) (g = lane % 16, q4 = lane / 16) then has the scores of tokens 16 q4 .. 16 q4 + 15.
+//    (The scaled 4-bit product, with the query as the sum of two 8-bit rows, needs no conversions, but it does not
+//    keep 32 bits of its sums: scores were off by up to 2^-13 of the sum of magnitudes where the query's components differ in size.)
+//  * The conversion yields two neighbouring components of a token.  For V the product wants pairs along the tokens: a token
+//    counts twice in its sum, once for each component, and P is held with zeros in the other place: O_even and O_odd are
+//    different columns.  (Bringing pairs of tokens together by byte permutes: 64 more instructions a chunk, as many products.)
 //  * P is multiplied in two parts, the upper 16 bits of its fp32 number and the upper 16 of what is left: 2^-16 off
 //    instead of bf16's 2^-9 (which would add as much again to the error of the bf16 output).  Up to 4 query heads (GM = 4): 16
 //    columns are 4 heads x even, odd x the two parts; up to 8 (GM = 8): two products; up to 16: four.
@@ -25,9 +23,7 @@
 
 namespace {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef short i16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct q4_params {
   dec_params d;                          // (k, v, packets, gen are not used)
@@ -35,12 +31,11 @@ struct q4_params {
 };
 
 // A chunk's registers.  Rows behind the last attended token are not read (a buffer load answers zeros).
-//   k   head_dim 128: 32 components (32 q4 ..) of token 4g + T; head_dim 64: 32 components (32 (q4 % 2) ..) of token
-//       4g + 2i + q4 / 2, two tiles in a register, the upper half of the lanes having the odd one
-//   ks  the scales of tokens 4g .. 4g + 3 for these components
+//   k   head_dim / 4 components ((head_dim / 4) q4 ..) of token 4g + T;  ks  the scales of tokens 4g .. 4g + 3 for them
 //   v   head_dim / 16 components of tokens 16 q4 + j;  vs  their 16 scales
-template <int D>
-struct q4_chunk { u32x4 k[D / 32]; uint32_t v[16]; uint32_t ks; u32x4 vs; };
+template <int D> struct q4_chunk;
+template <> struct q4_chunk<128> { u32x4 k[4]; uint32_t v[16]; uint32_t ks; u32x4 vs; };
+template <> struct q4_chunk<64> { u32x2 k[4]; uint32_t v[16]; uint32_t ks; u32x4 vs; };
 
 template <int D>
 __device__ __forceinline__ void q4_issue(q4_chunk<D>& c, const q4_params& p, int page, int kvh, int sub, int n_tok, int g, int q4) {
@@ -51,65 +46,19 @@ __device__ __forceinline__ void q4_issue(q4_chunk<D>& c, const q4_params& p, int
   const dec_buf kb = dec_buffer(p.k + data, n_tok * ROW), vb = dec_buffer(p.v + data, n_tok * ROW);
   const int scales = (D / 32 - 1) * p.d.B + CH;
   const dec_buf ksb = dec_buffer(p.ks + scale, scales), vsb = dec_buffer(p.vs + scale, scales);
-  if constexpr (D == 128) {
-    c.ks = __builtin_amdgcn_raw_buffer_load_b32(ksb, q4 * p.d.B + 4 * g, 0, 0);
+  c.ks = __builtin_amdgcn_raw_buffer_load_b32(ksb, (D == 128 ? q4 : q4 >> 1) * p.d.B + 4 * g, 0, 0);
 #pragma unroll
-    for (int T = 0; T < 4; ++T) c.k[T] = dec_load16(kb, 4 * g * ROW + 16 * q4, T * ROW);
-    c.vs = dec_load16(vsb, (g >> 2) * p.d.B + 16 * q4, 0);
+  for (int T = 0; T < 4; ++T) {
+    if constexpr (D == 128) c.k[T] = dec_load16(kb, 4 * g * ROW + 16 * q4, T * ROW);
+    else c.k[T] = __builtin_amdgcn_raw_buffer_load_b64(kb, 4 * g * ROW + 8 * q4 + T * ROW, 0, 0);
+  }
+  c.vs = dec_load16(vsb, (D == 128 ? g >> 2 : g >> 3) * p.d.B + 16 * q4, 0);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) c.v[j] = __builtin_amdgcn_raw_buffer_load_b32(vb, 16 * q4 * ROW + 4 * g + j * ROW, 0, 0);
-  } else {
-    c.ks = __builtin_amdgcn_raw_buffer_load_b32(ksb, (q4 & 1) * p.d.B + 4 * g, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) c.k[i] = dec_load16(kb, (4 * g + (q4 >> 1)) * ROW + 16 * (q4 & 1), 2 * i * ROW);
-    c.vs = dec_load16(vsb, (g >> 3) * p.d.B + 16 * q4, 0);
-#pragma unroll
-    for (int j = 0; j < 16; ++j) c.v[j] = __builtin_amdgcn_raw_buffer_load_b16(vb, 16 * q4 * ROW + 2 * g + j * ROW, 0, 0);
+  for (int j = 0; j < 16; ++j) {
+    if constexpr (D == 128) c.v[j] = __builtin_amdgcn_raw_buffer_load_b32(vb, 16 * q4 * ROW + 4 * g + j * ROW, 0, 0);
+    else c.v[j] = __builtin_amdgcn_raw_buffer_load_b16(vb, 16 * q4 * ROW + 2 * g + j * ROW, 0, 0);
   }
   __builtin_amdgcn_sched_barrier(0);       // every load is under way before the first product
-}
-
-// The query as the sum of two e4m3 rows.  Lane (g, q4) supplies components 16 q4 .. 16 q4 + 15 and, at head_dim 128, 64 + those, of
-// its column's head (the product's k index of an 8-bit operand; the scale of 32 components is the same for all).
-template <int D>
-struct q4_query { uint32_t hi[D / 16], lo[D / 16]; int s_hi, s_lo; };
-template <int D>
-__device__ __forceinline__ q4_query<D> q4_split_query(const u32x4 (&x)[D / 32]) {
-  constexpr int N = D / 16;
-  q4_query<D> q;
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < 2 * N; ++i) {
-    const uint32_t w = x[i / 4][i % 4];
-    amax = max(amax, max((w & 0x7fffu) << 16, w & 0x7fff0000u));
-  }
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16));
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
-  // the largest component lands in [2^7, 2^8); what the first part leaves is at most 2^3 and is held 2^5 finer
-  const int e = (int)(amax >> 23);
-  q.s_hi = e == 255 ? 255 : (e < 12 ? 5 : e - 7);        // (infinities and NaN: no score is a number)
-  q.s_lo = e == 255 ? 255 : q.s_hi - 5;
-  const float s_hi = q4_scale(q.s_hi), s_lo = q4_scale(q.s_lo);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t w0 = x[i / 2][2 * i % 4], w1 = x[i / 2][2 * i % 4 + 1];
-    i16x2 a = {0, 0}, b = {0, 0};
-    a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(q4_bf16x2, w0), s_hi, false);
-    a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(q4_bf16x2, w1), s_hi, true);
-    q.hi[i] = __builtin_bit_cast(uint32_t, a);
-    const f32x2 u = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(q.hi[i], s_hi, false), v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(q.hi[i], s_hi, true);
-    b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, __builtin_bit_cast(float, w0 << 16) - u[0], __builtin_bit_cast(float, w0 & 0xffff0000u) - u[1], s_lo, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, __builtin_bit_cast(float, w1 << 16) - v[0], __builtin_bit_cast(float, w1 & 0xffff0000u) - v[1], s_lo, true);
-    q.lo[i] = __builtin_bit_cast(uint32_t, b);
-  }
-  return q;
-}
-// S += K tile x the query: 4-bit rows with the scales in byte SEL of `ks`
-template <int SEL>
-__device__ __forceinline__ f32x4 q4_score(const u32x4& k, int ks, const i32x8& hi, const i32x8& lo, int s_hi, int s_lo, f32x4 S) {
-  const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-  S = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, hi, S, 4, 0, SEL, ks, 0, s_hi);
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, lo, S, 4, 0, SEL, ks, 0, s_lo);
 }
 
 // byte BYTE of a word of scales as the conversions want it: they look at the exponent's bits only, so what else is shifted
@@ -117,6 +66,20 @@ __device__ __forceinline__ f32x4 q4_score(const u32x4& k, int ks, const i32x8& h
 template <int BYTE>
 __device__ __forceinline__ float q4_scale_byte(uint32_t word) {
   return __builtin_bit_cast(float, BYTE == 3 ? word >> 1 : word << (23 - 8 * BYTE));
+}
+
+// A tile of scores: step s of the product is components (head_dim / 4) q4 + 8 s ..
+template <int D, int T>
+__device__ __forceinline__ f32x4 q4_score(const q4_chunk<D>& c, const bf16x8 (&qf)[D / 32]) {
+  const float sc = q4_scale_byte<T>(c.ks);
+  f32x4 S = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    const uint32_t w = c.k[T][s];
+    const u32x4 a = {q4_expand<0>(w, sc), q4_expand<1>(w, sc), q4_expand<2>(w, sc), q4_expand<3>(w, sc)};
+    S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), qf[s], S, 0, 0, 0);
+  }
+  return S;
 }
 
 // A lane's place among the columns
@@ -129,28 +92,9 @@ struct q4_column {
 
 // One online-softmax update with the chunk.
 template <int D, int GM>
-__device__ __forceinline__ void q4_consume(q4_chunk<D>& c, const q4_query<D>& q, int n_tok, float c2, int g, int q4,
+__device__ __forceinline__ void q4_consume(q4_chunk<D>& c, const bf16x8 (&qf)[D / 32], int n_tok, float c2, int g, int q4,
                                            float& m_run, float& l_run, f32x4 (&O)[GM == 16 ? 2 : 1][D / 32]) {
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  f32x4 S[4];
-  if constexpr (D == 128) {
-    i32x8 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { hi[i] = (int)q.hi[i]; lo[i] = (int)q.lo[i]; }
-    S[0] = q4_score<0>(c.k[0], (int)c.ks, hi, lo, q.s_hi, q.s_lo, zero);
-    S[1] = q4_score<1>(c.k[1], (int)c.ks, hi, lo, q.s_hi, q.s_lo, zero);
-    S[2] = q4_score<2>(c.k[2], (int)c.ks, hi, lo, q.s_hi, q.s_lo, zero);
-    S[3] = q4_score<3>(c.k[3], (int)c.ks, hi, lo, q.s_hi, q.s_lo, zero);
-  } else {
-    // a register has two tokens' rows; the other one's is multiplied by zeros, with a scale that is a number
-    const i32x8 hi0 = {(int)q.hi[0], (int)q.hi[1], (int)q.hi[2], (int)q.hi[3], 0, 0, 0, 0}, lo0 = {(int)q.lo[0], (int)q.lo[1], (int)q.lo[2], (int)q.lo[3], 0, 0, 0, 0};
-    const i32x8 hi1 = {0, 0, 0, 0, (int)q.hi[0], (int)q.hi[1], (int)q.hi[2], (int)q.hi[3]}, lo1 = {0, 0, 0, 0, (int)q.lo[0], (int)q.lo[1], (int)q.lo[2], (int)q.lo[3]};
-    const int ks0 = q4 < 2 ? (int)c.ks : 0, ks1 = q4 < 2 ? 0 : (int)c.ks;
-    S[0] = q4_score<0>(c.k[0], ks0, hi0, lo0, q.s_hi, q.s_lo, zero);
-    S[1] = q4_score<1>(c.k[0], ks1, hi1, lo1, q.s_hi, q.s_lo, zero);
-    S[2] = q4_score<2>(c.k[1], ks0, hi0, lo0, q.s_hi, q.s_lo, zero);
-    S[3] = q4_score<3>(c.k[1], ks1, hi1, lo1, q.s_hi, q.s_lo, zero);
-  }
+  f32x4 S[4] = {q4_score<D, 0>(c, qf), q4_score<D, 1>(c, qf), q4_score<D, 2>(c, qf), q4_score<D, 3>(c, qf)};
   // ---- S[T][r] is token 16 q4 + 4 r + T of this lane's head ----
   if (n_tok < CH) {                        // uniform: the sequence's last chunk
     const int left = n_tok - 16 * q4;
@@ -263,11 +207,12 @@ __device__ __forceinline__ void q4_stash(float* s_o, int wave, int G, int head, 
   }
 }
 
-// D: head_dim; GM: query heads that fit the columns; NWV: wavefronts of a workgroup
-template <int D, int GM, int NWV>
-__global__ __launch_bounds__(64 * NWV, GM == 16 ? 2 : 4) void pa_decode_q4_kernel(q4_params p) {
-  __shared__ float s_m[NWV][MAXG], s_l[NWV][MAXG];
-  extern __shared__ __attribute__((aligned(16))) float s_o[];    // [NWV][G][D/32][OROW]
+// D: head_dim; GM: query heads that fit the columns.  (Four or sixteen wavefronts instead of eight: one sequence 7.4 or 8.1 us
+// instead of 6.4; 1024 pairs level with four.)
+template <int D, int GM>
+__global__ __launch_bounds__(64 * NW, GM == 16 ? 2 : 4) void pa_decode_q4_kernel(q4_params p) {
+  __shared__ float s_m[NW][MAXG], s_l[NW][MAXG];
+  extern __shared__ __attribute__((aligned(16))) float s_o[];    // [NW][G][D/32][OROW]
   const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, g = lane & 15, q4 = lane >> 4;
@@ -275,10 +220,10 @@ __global__ __launch_bounds__(64 * NWV, GM == 16 ? 2 : 4) void pa_decode_q4_kerne
   const q4_column<GM> col(g);
 
   const int len = p.d.kv_len[b];
-  u32x4 qx[D / 32];
+  bf16x8 qf[D / 32];
   const dec_buf qb = dec_buffer(p.d.q + ((int64_t)b * p.d.hq + (int64_t)kvh * G) * D, G * 2 * D);    // (no such head: zeros)
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) qx[i] = dec_load16(qb, col.head * 2 * D + 32 * q4, 16 * (i & 1) + 128 * (i >> 1));
+  for (int s = 0; s < D / 32; ++s) qf[s] = __builtin_bit_cast(bf16x8, dec_load16(qb, col.head * 2 * D + (D / 2) * q4, 16 * s));
   const dec_row row = dec_row_of(p.d, len);
   const int n_slots = len > 0 ? row.n_slots : 0;                 // an empty sequence attends nothing
 
@@ -301,10 +246,9 @@ __global__ __launch_bounds__(64 * NWV, GM == 16 ? 2 : 4) void pa_decode_q4_kerne
   // (The next chunk requested before this one is used, in registers of its own: no gain, 40 to 100 registers more.)
   int slot = wave * p.d.splits + split;
   int n_tok = request(slot);
-  const q4_query<D> q = q4_split_query<D>(qx);                   // (while the chunk is on its way)
   while (n_tok > 0) {
-    q4_consume<D, GM>(c, q, n_tok, p.d.c2, g, q4, m_run, l_run, O);
-    n_tok = request(slot += NWV * p.d.splits);
+    q4_consume<D, GM>(c, qf, n_tok, p.d.c2, g, q4, m_run, l_run, O);
+    n_tok = request(slot += NW * p.d.splits);
   }
 
   // ---- the wavefronts' partials meet in LDS ----
@@ -322,14 +266,14 @@ __global__ __launch_bounds__(64 * NWV, GM == 16 ? 2 : 4) void pa_decode_q4_kerne
     if constexpr (GM == 16) q4_stash<D>(s_o, wave, G, col.head, true, q4, O[1]);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < G * D; e += 64 * NWV) {
+  for (int e = threadIdx.x; e < G * D; e += 64 * NW) {
     const int gg = e / D, d = e % D;
     float M = -INFINITY, L = 0.f, acc = 0.f;
 #pragma unroll
-    for (int w = 0; w < NWV; ++w) M = fmaxf(M, s_m[w][gg]);
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w][gg]);
     const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int w = 0; w < NWV; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float wt = __builtin_amdgcn_exp2f(s_m[w][gg] - ref);
       L = fmaf(wt, s_l[w][gg], L);
       acc = fmaf(wt, s_o[q4_o_at<D>(w, G, gg, d)], acc);
@@ -391,11 +335,11 @@ __global__ __launch_bounds__(64) void pa_decode_q4_merge_kernel(dec_params p) {
   if (p.lse && lane == 0) p.lse[h] = (M + log2f(L)) * 0.69314718055994530942f;
 }
 
-// Workgroups of a (sequence, KV head).  One takes about 1.4 us for each round of its eight wavefronts' chunks, and a second kernel
-// to add up the partials costs 2.5 to 3: a row is cut into parts of one round, as far as there are compute units for them, where
-// that saves three rounds.  us, rows of 24 / 40 / 64 / 128 / 256 / 1000 chunks, 8 pairs, one workgroup 9.9 / 12.9 / 17.1 / 28.0 / 49.6 / 182,
-// four 9.5 / 10.2 / 11.3 / 14.3 / 20.2 / 52.7, by this rule 9.9 / 9.8 / 10.2 / 11.0 / 11.9 / 20.0; 128 pairs, one 10.5 / 14.6 /
-// 19.6 / 32.1 / 62.3 / 271, two 11.0 / 14.5 / 18.8 / 29.4 / 51.7 / 230, four 13.3 / 16.4 / 20.3 / 30.2 / 52.4 / 235.
+// Workgroups of a (sequence, KV head).  One takes about 1.7 us for each round of its eight wavefronts' chunks, and a second kernel
+// to add up the partials costs 2 to 3: a row is cut into parts of one round, as far as there are compute units for them, where
+// that saves two rounds.  us, rows of 24 / 40 / 64 / 128 / 256 / 1000 chunks, 8 pairs, one workgroup 9.9 / 13.3 / 19.0 / 33.2 / 61.3 / 234,
+// four 8.9 / 9.6 / 11.2 / 15.0 / 22.2 / 67.6, parts of one round (from 40 on) 9.2 / 9.6 / 10.3 / 11.4 / 20.2; 128 pairs, one 10.4 / 15.0 / 21.5 /
+// 37.0 / 75.8 / 308, two 10.5 / 14.8 / 19.3 / 29.7 / 52.6 / 233, four 12.2 / 16.2 / 20.0 / 30.8 / 55.5 / 237; 13 chunks, 8 pairs, one 6.4, two 8.3.
 int32_t q4_splits(const powattn_pattern* pattern, int32_t batch, int32_t hkv, int64_t capacity) {
   const int32_t mk = powattn_max_k(pattern, capacity);
   if (mk < 1) return 0;
@@ -405,38 +349,24 @@ int32_t q4_splits(const powattn_pattern* pattern, int32_t batch, int32_t hkv, in
   const int64_t room = n_cu / ((int64_t)batch * hkv);
   int64_t s = rounds < room ? rounds : room;
   if (s > 256) s = 256;
-  if (s < 2 || rounds - (rounds + s - 1) / s < 3) return 1;
+  if (s < 2 || rounds - (rounds + s - 1) / s < 2) return 1;
   return (int32_t)s;
 }
 
-template <int D, int GM, int NWV>
-int launch_as(const q4_params& p, int batch, hipStream_t stream) {
+template <int D, int GM>
+int launch_q4(const q4_params& p, int batch, hipStream_t stream) {
   static std::atomic<unsigned long long> attr_done{0};
-  constexpr auto lds = [](int G) { return dec_o_bytes<D>(G) / NW * NWV; };
-  if (int st = pa_allow_dynamic_lds(reinterpret_cast<const void*>(&pa_decode_q4_kernel<D, GM, NWV>), lds(GM), attr_done)) return st;
+  if (int st = pa_allow_dynamic_lds(reinterpret_cast<const void*>(&pa_decode_q4_kernel<D, GM>), dec_o_bytes<D>(GM), attr_done)) return st;
   const dim3 grid((uint32_t)p.d.splits, (uint32_t)p.d.hkv, (uint32_t)batch);
-  hipLaunchKernelGGL((pa_decode_q4_kernel<D, GM, NWV>), grid, dim3(64 * NWV), lds(p.d.G), stream, p);
+  hipLaunchKernelGGL((pa_decode_q4_kernel<D, GM>), grid, dim3(64 * NW), dec_o_bytes<D>(p.d.G), stream, p);
   if (int st = pa_note_hip(hipGetLastError())) return st;
   if (p.d.splits == 1) return POWATTN_OK;
   hipLaunchKernelGGL((pa_decode_q4_merge_kernel<D>), dim3((uint32_t)p.d.hq, (uint32_t)batch), dim3(64), 0, stream, p.d);
   return pa_note_hip(hipGetLastError());
 }
-// Four wavefronts instead of eight where every compute unit has two pairs of four rounds or less: more of them are under way, so
-// that one's start and end run under the others' chunks (us, 1024 pairs 20.0 / 21.0, 512 pairs 12.6 / 13.3; 512 pairs of 56 chunks 33.0 /
-// 32.3, 256 pairs 10.8 / 9.6; head_dim 64, 512 pairs 9.9 / 9.5).
-template <int D, int GM>
-int launch_q4(const q4_params& p, int batch, int64_t chunks, hipStream_t stream) {
-  int n_cu = 1;
-  pa_current_device(nullptr, &n_cu);
-  if constexpr (D == 128)
-    if (p.d.splits == 1 && chunks <= 2 * NW && (int64_t)batch * p.d.hkv >= 2 * (int64_t)n_cu) return launch_as<D, GM, NW / 2>(p, batch, stream);
-  return launch_as<D, GM, NW>(p, batch, stream);
-}
 template <int D>
-int launch_d(const q4_params& p, int batch, int64_t chunks, hipStream_t stream) {
-  if (p.d.G <= 4) return launch_q4<D, 4>(p, batch, chunks, stream);
-  if (p.d.G <= 8) return launch_q4<D, 8>(p, batch, chunks, stream);
-  return launch_q4<D, 16>(p, batch, chunks, stream);
+int launch_d(const q4_params& p, int batch, hipStream_t stream) {
+  return p.d.G <= 4 ? launch_q4<D, 4>(p, batch, stream) : p.d.G <= 8 ? launch_q4<D, 8>(p, batch, stream) : launch_q4<D, 16>(p, batch, stream);
 }
 
 }  // namespace
@@ -492,6 +422,5 @@ extern "C" int powattn_decode_paged_q4(const powattn_pattern* pattern, const voi
   d.c2 = scale * 1.44269504088896340736f;
   d.block_table = d_block_table; d.table_stride = table_stride; d.last_page = (int32_t)n_pages - 1;
   hipStream_t stream = (hipStream_t)hip_stream;
-  const int64_t chunks = (int64_t)powattn_max_k(pattern, capacity) * d.subs;
-  return head_dim == 128 ? launch_d<128>(p, batch, chunks, stream) : launch_d<64>(p, batch, chunks, stream);
+  return head_dim == 128 ? launch_d<128>(p, batch, stream) : launch_d<64>(p, batch, stream);
 }

@@ -164,3 +164,20 @@ def test_as_the_decode_step_over_bf16_pages():
     tol = 2.0 ** -7 * np.abs(o4) + (2.0 ** -9 + 2.0 ** -11) * 12
     assert (np.abs(o.double().cpu().numpy() - o4) <= tol).all()
     assert np.abs(lse.double().cpu().numpy() - lse4).max() <= 2.0 ** -12
+
+
+def test_scores_are_summed_in_32_bits():
+    # queries whose components differ by 2^13 and rows of one to three keys, whose log-sum-exp is hardly more than a score.  128
+    # products of bf16 numbers, exact in fp32: 128 roundings of 2^-24 of the sum of magnitudes, and 2^-20 for exp, log and scale
+    pat, b, hq, hkv, d = pa.Pattern(64, 2, 1), 24, 8, 2, 128
+    lens = [1 + i % 3 for i in range(b)]
+    q, cache, table, (k, v) = make(pat, b, hq, hkv, d, lens, 16)
+    rng = np.random.default_rng(17)
+    q = (q.double() * torch.from_numpy(2.0 ** -rng.integers(0, 14, size=q.shape))).bfloat16()
+    _, lse = run(pat, q, cache, table, lens)
+    for i, n in enumerate(lens):
+        qi, ki = q[i].double().numpy(), k[i, :, :n].repeat(hq // hkv, 0)
+        s = (qi[:, None] * ki).sum(-1) / np.sqrt(d)
+        size = (np.abs(qi[:, None] * ki).sum(-1) / np.sqrt(d)).max(-1)
+        want = np.log(np.exp(s - s.max(-1, keepdims=True)).sum(-1)) + s.max(-1)
+        assert (np.abs(lse[i] - want) <= 2.0 ** -17 * size + 2.0 ** -20 * (1 + np.abs(want))).all()
