@@ -403,7 +403,8 @@ int powattn_backward(const powattn_pattern* pattern,
  *                     page is not in [0, n_pages)
  *   d_kv_len          device int32 [batch], out: s + n, as the decode calls take it
  *   d_n_taken         device int32 [1], out: the number of new pages of all sequences; more than n_free: the list was too short
- * The free list itself is not changed: the pages taken are its first d_n_taken[0].  The inputs may not overlap the outputs.
+ * The free list itself is not changed: the pages taken are its first d_n_taken[0].  The inputs may not overlap the
+ * outputs (d_kv_len in the place of d_q_start, for instance, is refused).
  * Limits: table_stride * block and n_pages * block below 2^31.
  * Errors: INVALID_ARG (q_rows above table_stride*block among them), UNSUPPORTED, HIP_ERROR.
  */
@@ -445,8 +446,8 @@ int powattn_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k,
  * Gradients of sum(q_out * d_q_out) + sum(k_out * d_k_out) of powattn_qk_norm_rope with the same inputs.
  *   d_q_out, d_k_out  device, contiguous, as q_out and k_out (what powattn_backward writes as dq and dk)
  *   dq, dk            device rows with strides of their own (host int64 [3]), so that they can be written into the gradient of
- *                     the projections' output; no two rows may overlap.  Rows r >= d_q_len[b] are not written, and nothing
- *                     of theirs is read
+ *                     the projections' output; no two rows may overlap, nor may they overlap the inputs.  Rows r >= d_q_len[b]
+ *                     are not written, and nothing of theirs is read
  *   dq_weight, dk_weight  device float [head_dim], whatever dtype is: the sums over all rows and heads, in a fixed order
  *   workspace         device, powattn_qk_norm_rope_backward_workspace_bytes(...) bytes, 256-byte aligned, contents ignored;
  *                     calls that may run at the same time must not share one

@@ -112,6 +112,10 @@ extern "C" int powattn_page_tables(const powattn_pattern* pattern, const int32_t
   if (!d_q_start || !d_q_len || !d_block_table || !d_slots || !d_kv_len || !d_n_taken) return POWATTN_INVALID_ARG;
   if (batch < 1 || q_rows < 1 || n_free < 0 || n_pages < 1 || table_stride < 1) return POWATTN_INVALID_ARG;
   if (n_free > 0 && !d_free_pages) return POWATTN_INVALID_ARG;
+  // (every workgroup reads the lengths of the sequences before its own, so an output in their place would change them under it)
+  const int32_t* out[] = {d_block_table, d_slots, d_kv_len, d_n_taken};
+  for (const int32_t* o : out)
+    if (o == d_q_start || o == d_q_len || (n_free > 0 && o == d_free_pages)) return POWATTN_INVALID_ARG;
   const int64_t capacity = (int64_t)table_stride * pattern->block;
   if (q_rows > capacity) return POWATTN_INVALID_ARG;
   if (capacity > 0x7fffffff || n_pages > 0x7fffffff / pattern->block) return POWATTN_UNSUPPORTED;   // slots and positions are 32-bit numbers

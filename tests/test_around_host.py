@@ -16,8 +16,8 @@ def L():
     return pa.lib()
 
 
-def _tables(L, pat=None, start=FAKE, n=FAKE, batch=4, rows=10, free=FAKE, n_free=9, n_pages=100, table=FAKE, stride=16, slots=FAKE,
-            kv_len=FAKE, taken=FAKE):
+def _tables(L, pat=None, start=FAKE, n=2 * FAKE, batch=4, rows=10, free=3 * FAKE, n_free=9, n_pages=100, table=4 * FAKE, stride=16,
+            slots=5 * FAKE, kv_len=6 * FAKE, taken=7 * FAKE):
     cp = (pat or pa.Pattern(64, 4, 1)).c()
     return L.powattn_page_tables(ctypes.byref(cp), start, n, batch, rows, free, n_free, n_pages, table, stride, slots, kv_len, taken,
                                  None)
@@ -29,11 +29,14 @@ def test_page_tables_argument_errors(L):
     for name in ("batch", "rows", "n_pages", "stride"):
         assert _tables(L, **{name: 0}) == pa.INVALID_ARG, name
     assert _tables(L, n_free=-1) == pa.INVALID_ARG
+    for out in ("table", "slots", "kv_len", "taken"):                          # an output in the place of an input
+        for where in (FAKE, 2 * FAKE, 3 * FAKE):
+            assert _tables(L, **{out: where}) == pa.INVALID_ARG, out
     assert _tables(L, rows=16 * 64 + 1) == pa.INVALID_ARG
     assert _tables(L, pat=pa.Pattern(0, 4, 1)) == pa.INVALID_ARG
     assert _tables(L, n_pages=2 ** 31 // 64) == pa.UNSUPPORTED                  # slots are 32-bit numbers
     assert _tables(L, stride=2 ** 25) == pa.UNSUPPORTED
-    assert L.powattn_page_tables(None, FAKE, FAKE, 4, 1, FAKE, 1, 1, FAKE, 1, FAKE, FAKE, FAKE, None) == pa.INVALID_ARG
+    assert L.powattn_page_tables(None, FAKE, 2 * FAKE, 4, 1, 3 * FAKE, 1, 1, 4 * FAKE, 1, 5 * FAKE, 6 * FAKE, 7 * FAKE, None) == pa.INVALID_ARG
 
 
 def _rope(L, q=FAKE, qs=STRIDES, k=FAKE, ks=STRIDES, qw=FAKE, kw=FAKE, inv=FAKE, rot=128, flags=0, qo=FAKE, ko=FAKE, batch=2, hq=4, hkv=2,

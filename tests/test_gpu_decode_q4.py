@@ -135,8 +135,8 @@ def test_lengths_and_pages_outside_are_clamped():
     assert np.array_equal(run(pat, q, cache, bad, [640])[0], run(pat, q, cache, good, [640])[0])
 
 
-def test_a_key_or_value_without_a_number():
-    pat = pa.Pattern(64, 2, 1)
+@pytest.mark.parametrize("pat", [pa.Pattern(64, 2, 1), pa.Pattern(64, 400, 1, 0)], ids=["one workgroup", "several"])
+def test_a_key_or_value_without_a_number(pat):
     for n in (200, 5000):
         q, cache, table, _ = make(pat, 2, 4, 2, 128, [n, n], 14)
         o, lse = run(pat, q, cache, table, [n, n])
