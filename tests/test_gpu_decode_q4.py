@@ -181,3 +181,28 @@ def test_scores_are_summed_in_32_bits():
         size = (np.abs(qi[:, None] * ki).sum(-1) / np.sqrt(d)).max(-1)
         want = np.log(np.exp(s - s.max(-1, keepdims=True)).sum(-1)) + s.max(-1)
         assert (np.abs(lse[i] - want) <= 2.0 ** -17 * size + 2.0 ** -20 * (1 + np.abs(want))).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(3, 1), (8, 1), (12, 2), (12, 1), (16, 1)])
+def test_heads_of_a_row_in_several_parts(d, hq, hkv):
+    check(pa.Pattern(64, 400, 1, 0), 2, hq, hkv, d, [5000, 1 + 64 * 9], seed=hq + d)
+
+
+def test_pages_beyond_32_bit_offsets():
+    pat, hq, hkv, d, n = pa.Pattern(1024, 2, 1), 8, 8, 128, 1500
+    cache = pa.cache_q4(pat, 8400, hkv, d)
+    assert cache.k.numel() > 2 ** 32
+    gen = torch.Generator().manual_seed(18)
+    k, v = (torch.randn((1, hkv, n, d), generator=gen).bfloat16().cuda() for _ in range(2))
+    q = torch.randn((1, hq, d), generator=gen).bfloat16()
+    table = torch.tensor([[8399, 8398]], dtype=torch.int32, device="cuda")
+    pos = torch.arange(n, device="cuda")
+    slots = (table[0, (pos // 1024)].long() * 1024 + pos % 1024).int().view(1, n)
+    pa.cache_store_q4(pat, k, v, cache, slots)
+    o, lse = pa.decode_paged_q4(pat, q.cuda(), cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"))
+    held = [t.double().cpu().numpy() for t in pa.cache_load_q4(pat, cache, table, n)]
+    want, want_lse = orc.decode(q.double().numpy(), *held, [n], oracle_pattern(pat))
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -12 * np.abs(held[1]).max()
+    assert (np.abs(o.double().cpu().numpy() - want) <= tol).all()
+    assert np.abs(lse.double().cpu().numpy() - want_lse).max() <= 2.0 ** -13

@@ -205,3 +205,14 @@ def test_a_large_call_is_its_parts(dtype, n):
         assert all(torch.equal(a[:, :, lo:hi], x) for a, x in zip(outs, got))
         got = pa.qk_norm_rope_backward(*parts, *w, inv, *(x[:, :, lo:hi].contiguous() for x in dy), q_start=start)
         assert all(torch.equal(a[:, :, lo:hi], x) for a, x in zip(grads[:2], got[:2]))
+
+
+def test_a_batch_without_rows():
+    q, k, w, inv = inputs("bf16", 2, 3, 1, 40, 64, 64, 61)
+    none = torch.zeros(2, dtype=torch.int32, device="cuda")
+    args = (on_gpu(q), on_gpu(k), w[0].cuda(), w[1].cuda(), inv.cuda())
+    for t in pa.qk_norm_rope(*args, q_len=none):
+        assert not t.any()
+    nan = [torch.full(x.shape, float("nan"), dtype=torch.bfloat16, device="cuda") for x in (q, k)]
+    for t in pa.qk_norm_rope_backward(*args, *nan, q_len=none):
+        assert not t.any()
