@@ -1,10 +1,11 @@
 // Rows of keys and values into the 4-bit cache and out of it (format: q4.h).
 //
-// Both move bytes and nothing else.  A lane has 8 components, 16 bytes in bf16 and 4 in the cache, four lanes share a scale.
-// Where there are rows enough, a lane has four consecutive ones: they mostly lie side by side in a page, and their scales
-// are one word then.  A workgroup looks its rows' slots (pages) up once and walks through heads, keys and values
-// together; the next head's rows are requested before the current one's are converted.  With few rows a lane has one, of the keys or
-// of the values.
+// Both move bytes and nothing else.  A lane has 8 components, 16 bytes in bf16 and 4 in the cache, four lanes share a scale, and a
+// wavefront takes consecutive rows, so that its pieces of a page are one stretch.  A workgroup looks its rows' slots (pages)
+// up once and walks through heads; the next head's rows are requested before the current one's are converted.
+// 37399 rows of 8 heads of 128: stored in 36.6 us (5.3 TB/s), loaded in 34.7 (5.6); 128 rows 3.3 and 3.2.
+// (Four consecutive rows of a lane, of keys and values both, whose scales are one word then: stored and loaded, 32 pieces of up to 2048 rows
+// 99 / 78 us, 4000 rows of 8 heads 14.1 / 13.6, 1000 10.8 / 6.6, 128 10.4 / 4.8.)
 #include "common.h"
 #include "q4.h"
 
@@ -31,87 +32,40 @@ __device__ __forceinline__ u32x4 q4_load8(const uint16_t* p) {
   for (int i = 0; i < 4; ++i) r[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
   return r;
 }
-// Four consecutive rows whose slots (positions) follow one another from a multiple of four on, which four rows of a page do
-template <int TOK>
-__device__ __forceinline__ bool q4_side_by_side(const int32_t (&slot)[TOK]) {
-  if constexpr (TOK != 4) return false;
-  else return slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3;
-}
 
-// D: head_dim; TOK: consecutive rows of a lane, of keys and of values (one: blockIdx.z says of which)
-template <int D, int TOK, bool VEC>
+// D: head_dim; blockIdx.z: keys or values
+template <int D, bool VEC>
 __global__ __launch_bounds__(THREADS) void pa_cache_store_q4_kernel(store_params p) {
-  constexpr int LPR = D / 8, NKV = TOK == 1 ? 1 : 2;        // lanes of a row
-  const int lane = threadIdx.x % LPR, kv0 = NKV == 1 ? blockIdx.z : 0;
-  const int64_t t0 = ((int64_t)blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR) * TOK;
+  constexpr int LPR = D / 8;                                // lanes of a row
+  const int lane = threadIdx.x % LPR, kv = blockIdx.z;
+  const int64_t t = (int64_t)blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR;
   const int h0 = blockIdx.y * p.per_chunk, h1 = min(h0 + p.per_chunk, p.hkv);
-  int32_t slot[TOK];
-  const uint16_t* from[NKV][TOK];
-  int64_t page[TOK]; int32_t off[TOK];
-  bool any = false;
+  const int32_t slot = t < p.n_tokens ? p.slots[t] : -1;
+  if (slot < 0 || slot >= p.n_slots) return;                // rows without a slot are not read (the lanes of a row stay together)
+  const unsigned b = (unsigned)t / (unsigned)p.rows, r = (unsigned)t - b * (unsigned)p.rows;
+  const unsigned page = (unsigned)slot / (unsigned)p.B, off = (unsigned)slot - page * (unsigned)p.B;
+  const uint16_t* from = p.in[kv].p + b * p.in[kv].sb + r * p.in[kv].sr + 8 * lane;
+  const int64_t sh = p.in[kv].sh;
+  u32x4 x = q4_load8<VEC>(from + h0 * sh), next = x;
+  for (int h = h0; h < h1; ++h, x = next) {
+    if (h + 1 < h1) next = q4_load8<VEC>(from + (h + 1) * sh);
+    uint32_t amax = 0;                                      // magnitudes order like their bits
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    slot[i] = t0 + i < p.n_tokens ? p.slots[t0 + i] : -1;
-    if (slot[i] >= p.n_slots) slot[i] = -1;                 // rows without a slot are not read
-    any = any || slot[i] >= 0;
-  }
-  if (!any) return;                                         // (the lanes of a row stay together)
-#pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    const unsigned t = (unsigned)(t0 + i), b = t / (unsigned)p.rows, r = t - b * (unsigned)p.rows;
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv) from[kv][i] = p.in[kv0 + kv].p + b * p.in[kv0 + kv].sb + r * p.in[kv0 + kv].sr + 8 * lane;
-    const unsigned pg = (unsigned)max(slot[i], 0) / (unsigned)p.B;
-    page[i] = (int64_t)pg * p.hkv;
-    off[i] = max(slot[i], 0) - (int)pg * p.B;
-  }
-  const bool together = q4_side_by_side<TOK>(slot);         // (a block is a multiple of 64 rows: they are in one page)
-  u32x4 x[NKV][TOK], next[NKV][TOK];
-  auto request = [&](u32x4 (&y)[NKV][TOK], int h) {
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv)
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) {
-        y[kv][i] = u32x4{0, 0, 0, 0};
-        if (slot[i] >= 0) y[kv][i] = q4_load8<VEC>(from[kv][i] + h * p.in[kv0 + kv].sh);
-      }
-  };
-  request(x, h0);
-  for (int h = h0; h < h1; ++h) {
-    if (h + 1 < h1) request(next, h + 1);
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv) {
-      uint32_t codes = 0;
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) {
-        const u32x4 y = x[kv][i];
-        uint32_t amax = 0;                                  // magnitudes order like their bits
-#pragma unroll
-        for (int e = 0; e < 4; ++e) amax = max(amax, max((y[e] & 0x7fffu) << 16, y[e] & 0x7fff0000u));
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
-        const uint32_t code = q4_scale_code(amax);
-        uint32_t word = 0;
-        if (code != 255u) {
-          const float scale = q4_scale(code);
-          word = q4_shrink<0>(word, y[0], scale);
-          word = q4_shrink<1>(word, y[1], scale);
-          word = q4_shrink<2>(word, y[2], scale);
-          word = q4_shrink<3>(word, y[3], scale);
-        }
-        codes |= code << (8 * i);
-        if (slot[i] < 0) continue;
-        const int64_t at = page[i] + h;
-        *reinterpret_cast<uint32_t*>(p.pages[kv0 + kv] + (at * p.B + off[i]) * (D / 2) + 4 * lane) = word;
-        if ((lane & 3) == 0 && !together) p.scales[kv0 + kv][(at * (D / 32) + (lane >> 2)) * p.B + off[i]] = (uint8_t)code;
-      }
-      if ((lane & 3) == 0 && together)
-        *reinterpret_cast<uint32_t*>(p.scales[kv0 + kv] + ((page[0] + h) * (D / 32) + (lane >> 2)) * p.B + off[0]) = codes;
+    for (int e = 0; e < 4; ++e) amax = max(amax, max((x[e] & 0x7fffu) << 16, x[e] & 0x7fff0000u));
+    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+    const uint32_t code = q4_scale_code(amax);
+    uint32_t word = 0;
+    if (code != 255u) {
+      const float scale = q4_scale(code);
+      word = q4_shrink<0>(word, x[0], scale);
+      word = q4_shrink<1>(word, x[1], scale);
+      word = q4_shrink<2>(word, x[2], scale);
+      word = q4_shrink<3>(word, x[3], scale);
     }
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv)
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) x[kv][i] = next[kv][i];
+    const int64_t at = (int64_t)page * p.hkv + h;
+    *reinterpret_cast<uint32_t*>(p.pages[kv] + (at * p.B + off) * (D / 2) + 4 * lane) = word;
+    if ((lane & 3) == 0) p.scales[kv][(at * (D / 32) + (lane >> 2)) * p.B + off] = (uint8_t)code;
   }
 }
 
@@ -122,69 +76,35 @@ struct load_params {
   int32_t n_tokens, rows, hkv, B, stride, last_page, capacity, per_chunk;
 };
 
-template <int D, int TOK>
+template <int D>
 __global__ __launch_bounds__(THREADS) void pa_cache_load_q4_kernel(load_params p) {
-  constexpr int LPR = D / 8, NKV = TOK == 1 ? 1 : 2;
-  const int lane = threadIdx.x % LPR, kv0 = NKV == 1 ? blockIdx.z : 0;
-  const int64_t t0 = ((int64_t)blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR) * TOK;
+  constexpr int LPR = D / 8;
+  const int lane = threadIdx.x % LPR, kv = blockIdx.z;
+  const int64_t t = (int64_t)blockIdx.x * (THREADS / LPR) + threadIdx.x / LPR;
   const int h0 = blockIdx.y * p.per_chunk, h1 = min(h0 + p.per_chunk, p.hkv);
-  int64_t page[TOK], to[TOK];
-  int32_t off[TOK], where[TOK];
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    where[i] = -1;
-    page[i] = to[i] = off[i] = 0;
-    if (t0 + i >= p.n_tokens) continue;
-    const unsigned t = (unsigned)(t0 + i), b = t / (unsigned)p.rows, r = t - b * (unsigned)p.rows;
-    int32_t s = p.start ? p.start[b] : 0, n = p.length ? p.length[b] : p.rows;
-    s = s < 0 ? 0 : (s > p.capacity ? p.capacity : s);
-    if (n > p.capacity - s) n = p.capacity - s;
-    if ((int32_t)r >= n) continue;
-    const unsigned pos = (unsigned)s + r, blk = pos / (unsigned)p.B;
-    int pg = p.table[(int64_t)b * p.stride + blk];
-    pg = pg < 0 ? 0 : (pg > p.last_page ? p.last_page : pg);             // a bad table gives wrong numbers, no stray access
-    page[i] = (int64_t)pg * p.hkv;
-    off[i] = (int32_t)(pos - blk * (unsigned)p.B);
-    where[i] = pg * p.B + off[i];
-    to[i] = ((int64_t)b * p.hkv * p.rows + r) * D + 8 * lane;
-    any = true;
-  }
-  if (!any) return;
-  const bool together = q4_side_by_side<TOK>(where);
-  uint32_t word[NKV][TOK], code[NKV][TOK], next_word[NKV][TOK], next_code[NKV][TOK];
-  auto request = [&](uint32_t (&w)[NKV][TOK], uint32_t (&c)[NKV][TOK], int h) {
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv) {
-      if (together) c[kv][0] = *reinterpret_cast<const uint32_t*>(p.scales[kv0 + kv] + ((page[0] + h) * (D / 32) + (lane >> 2)) * p.B + off[0]);
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) {
-        if (where[i] < 0) continue;
-        const int64_t at = page[i] + h;
-        w[kv][i] = *reinterpret_cast<const uint32_t*>(p.pages[kv0 + kv] + (at * p.B + off[i]) * (D / 2) + 4 * lane);
-        if (!together) c[kv][i] = p.scales[kv0 + kv][(at * (D / 32) + (lane >> 2)) * p.B + off[i]];
-      }
-    }
+  if (t >= p.n_tokens) return;
+  const unsigned b = (unsigned)t / (unsigned)p.rows, r = (unsigned)t - b * (unsigned)p.rows;
+  int32_t s = p.start ? p.start[b] : 0, n = p.length ? p.length[b] : p.rows;
+  s = s < 0 ? 0 : (s > p.capacity ? p.capacity : s);
+  if (n > p.capacity - s) n = p.capacity - s;
+  if ((int32_t)r >= n) return;
+  const unsigned pos = (unsigned)s + r, blk = pos / (unsigned)p.B, off = pos - blk * (unsigned)p.B;
+  int page = p.table[(int64_t)b * p.stride + blk];
+  page = page < 0 ? 0 : (page > p.last_page ? p.last_page : page);       // a bad table gives wrong numbers, no stray access
+  uint16_t* to = p.out[kv] + ((int64_t)b * p.hkv * p.rows + r) * D + 8 * lane;
+  uint32_t word, code, next_word = 0, next_code = 0;
+  auto request = [&](uint32_t& w, uint32_t& c, int h) {
+    const int64_t at = (int64_t)page * p.hkv + h;
+    w = *reinterpret_cast<const uint32_t*>(p.pages[kv] + (at * p.B + off) * (D / 2) + 4 * lane);
+    c = p.scales[kv][(at * (D / 32) + (lane >> 2)) * p.B + off];
   };
   request(word, code, h0);
-  for (int h = h0; h < h1; ++h) {
+  for (int h = h0; h < h1; ++h, word = next_word, code = next_code) {
     if (h + 1 < h1) request(next_word, next_code, h + 1);
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv)
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) {
-        if (where[i] < 0) continue;
-        const float scale = q4_scale(together ? code[kv][0] >> (8 * i) & 255u : code[kv][i]);
-        const uint32_t w = word[kv][i];
-        const u32x4 x = {q4_expand<0>(w, scale), q4_expand<1>(w, scale), q4_expand<2>(w, scale), q4_expand<3>(w, scale)};
-        u32x4* to_row = reinterpret_cast<u32x4*>(p.out[kv0 + kv] + to[i] + (int64_t)h * p.rows * D);
-        if constexpr (TOK == 4) __builtin_nontemporal_store(x, to_row);      // (us, 32 pieces of up to 2048 rows: 45 -> 40)
-        else *to_row = x;
-      }
-#pragma unroll
-    for (int kv = 0; kv < NKV; ++kv)
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) { word[kv][i] = next_word[kv][i]; code[kv][i] = next_code[kv][i]; }
+    const float scale = q4_scale(code);
+    const u32x4 x = {q4_expand<0>(word, scale), q4_expand<1>(word, scale), q4_expand<2>(word, scale), q4_expand<3>(word, scale)};
+    // past the caches: stored and loaded, us, 32 pieces of up to 2048 rows 78 / 96 through them, 1000 rows 6.6 / 6.7, 128 rows level
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to + (int64_t)h * p.rows * D));
   }
 }
 
@@ -199,20 +119,16 @@ int check_cache(const powattn_pattern* pattern, int32_t batch, int32_t hkv, int6
   return POWATTN_OK;
 }
 
-// The launch: four rows of a lane where that leaves a workgroup for every compute unit, else one; as many heads of a workgroup as
-// leave eight workgroups for every compute unit.
-struct q4_launch { int tok; int32_t per_chunk; dim3 grid; };
-bool launch_of(q4_launch& l, int64_t n_tokens, int32_t hkv, int32_t head_dim) {
+// As many heads of a workgroup as leave eight workgroups for every compute unit.
+bool grid_of(dim3& grid, int32_t& per_chunk, int64_t n_tokens, int32_t hkv, int32_t head_dim) {
   int n_cu = 1;
   pa_current_device(nullptr, &n_cu);
-  const int64_t side = THREADS / (head_dim / 8);
-  l.tok = n_tokens * hkv >= 4 * side * n_cu ? 4 : 1;
-  const int64_t groups = (n_tokens + side * l.tok - 1) / (side * l.tok);
+  const int64_t side = THREADS / (head_dim / 8), groups = (n_tokens + side - 1) / side;
   int64_t chunks = (8 * (int64_t)n_cu + groups - 1) / groups;
   if (chunks > hkv) chunks = hkv;
-  l.per_chunk = (int32_t)((hkv + chunks - 1) / chunks);
-  l.grid = dim3((uint32_t)groups, (uint32_t)((hkv + l.per_chunk - 1) / l.per_chunk), l.tok == 1 ? 2 : 1);
-  return (int64_t)l.grid.x * l.grid.y * l.grid.z <= 0xffffffffLL / THREADS;      // a launch has fewer than 2^32 threads
+  per_chunk = (int32_t)((hkv + chunks - 1) / chunks);
+  grid = dim3((uint32_t)groups, (uint32_t)((hkv + per_chunk - 1) / per_chunk), 2);
+  return (int64_t)grid.x * grid.y * 2 <= 0xffffffffLL / THREADS;      // a launch has fewer than 2^32 threads
 }
 
 }  // namespace
@@ -237,18 +153,12 @@ extern "C" int powattn_cache_store_q4(const powattn_pattern* pattern, const void
   p.n_slots = (int32_t)(n_pages * pattern->block);
   bool vec = (((uintptr_t)k | (uintptr_t)v) & 15u) == 0;
   for (int i = 0; i < 3; ++i) vec = vec && k_strides[i] % 8 == 0 && v_strides[i] % 8 == 0;
-  q4_launch l;
-  if (!launch_of(l, p.n_tokens, n_kv_heads, head_dim)) return POWATTN_UNSUPPORTED;
-  p.per_chunk = l.per_chunk;
+  dim3 grid;
+  if (!grid_of(grid, p.per_chunk, p.n_tokens, n_kv_heads, head_dim)) return POWATTN_UNSUPPORTED;
   hipStream_t stream = (hipStream_t)hip_stream;
-#define STORE(D, TOK, VEC) hipLaunchKernelGGL((pa_cache_store_q4_kernel<D, TOK, VEC>), l.grid, dim3(THREADS), 0, stream, p)
-  if (head_dim == 128) {
-    if (l.tok == 4) { if (vec) STORE(128, 4, true); else STORE(128, 4, false); }
-    else { if (vec) STORE(128, 1, true); else STORE(128, 1, false); }
-  } else {
-    if (l.tok == 4) { if (vec) STORE(64, 4, true); else STORE(64, 4, false); }
-    else { if (vec) STORE(64, 1, true); else STORE(64, 1, false); }
-  }
+#define STORE(D, VEC) hipLaunchKernelGGL((pa_cache_store_q4_kernel<D, VEC>), grid, dim3(THREADS), 0, stream, p)
+  if (head_dim == 128) { if (vec) STORE(128, true); else STORE(128, false); }
+  else { if (vec) STORE(64, true); else STORE(64, false); }
 #undef STORE
   return pa_note_hip(hipGetLastError());
 }
@@ -272,13 +182,10 @@ extern "C" int powattn_cache_load_q4(const powattn_pattern* pattern, const void*
   p.table = d_block_table; p.start = d_start; p.length = d_length;
   p.n_tokens = (int32_t)(batch * rows); p.rows = (int32_t)rows; p.hkv = n_kv_heads; p.B = pattern->block;
   p.stride = table_stride; p.last_page = (int32_t)n_pages - 1; p.capacity = (int32_t)capacity;
-  q4_launch l;
-  if (!launch_of(l, p.n_tokens, n_kv_heads, head_dim)) return POWATTN_UNSUPPORTED;
-  p.per_chunk = l.per_chunk;
+  dim3 grid;
+  if (!grid_of(grid, p.per_chunk, p.n_tokens, n_kv_heads, head_dim)) return POWATTN_UNSUPPORTED;
   hipStream_t stream = (hipStream_t)hip_stream;
-#define LOAD(D, TOK) hipLaunchKernelGGL((pa_cache_load_q4_kernel<D, TOK>), l.grid, dim3(THREADS), 0, stream, p)
-  if (head_dim == 128) { if (l.tok == 4) LOAD(128, 4); else LOAD(128, 1); }
-  else { if (l.tok == 4) LOAD(64, 4); else LOAD(64, 1); }
-#undef LOAD
+  if (head_dim == 128) hipLaunchKernelGGL((pa_cache_load_q4_kernel<128>), grid, dim3(THREADS), 0, stream, p);
+  else hipLaunchKernelGGL((pa_cache_load_q4_kernel<64>), grid, dim3(THREADS), 0, stream, p);
   return pa_note_hip(hipGetLastError());
 }

@@ -3,7 +3,8 @@
 //   du = the rotation back of dy;  dw = sum over all rows of du n;  dn = w du;  dx = r (dn - n mean(dn n))
 // with pairs (i, i + rot_dim / 2), or (2i, 2i + 1) where POWATTN_ROPE_INTERLEAVED is set.
 //
-// Bound by memory: 2 (gradients: 3) passes over the tensors.  A row of head_dim components belongs to 8 (head_dim 64: 4)
+// Bound by memory: 2 (gradients: 3) passes over the tensors (32768 rows of 32 heads of 128 in bf16: 102 us, 5.2 TB/s; gradients 171,
+// 4.7).  A row of head_dim components belongs to 8 (head_dim 64: 4)
 // lanes, 16 components each in two pieces of 8, chosen so that both halves of a pair are in one lane; a wavefront has 8
 // (16) consecutive tokens of a head, and walks through the heads with the same angles.  An angle is the exact product of
 // the position and the frequency, reduced to a part of a turn in 64 bits (in 32 bits a position of a million is known to a
