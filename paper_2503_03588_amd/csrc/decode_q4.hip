@@ -339,7 +339,7 @@ __global__ __launch_bounds__(64) void pa_decode_q4_merge_kernel(dec_params p) {
 // Workgroups of a (sequence, KV head).  One takes about 1.7 us for each round of its eight wavefronts' chunks, and a second kernel
 // to add up the partials costs 2 to 3: a row is cut into parts of one round, as far as there are compute units for them, where
 // that saves two rounds.  us, rows of 24 / 40 / 64 / 128 / 256 / 1000 chunks, 8 pairs, one workgroup 9.9 / 13.3 / 19.0 / 33.2 / 61.3 / 234,
-// four 8.9 / 9.6 / 11.2 / 15.0 / 22.2 / 67.6, parts of one round (from 40 on) 9.2 / 9.6 / 10.3 / 11.4 / 20.2; 128 pairs, one 10.4 / 15.0 / 21.5 /
+// four 8.9 / 9.6 / 11.2 / 15.0 / 22.2 / 67.6, parts of one round 9.1 / 9.3 / 9.6 / 10.3 / 11.3 / 20.3; 128 pairs, one 10.4 / 15.0 / 21.5 /
 // 37.0 / 75.8 / 308, two 10.5 / 14.8 / 19.3 / 29.7 / 52.6 / 233, four 12.2 / 16.2 / 20.0 / 30.8 / 55.5 / 237; 13 chunks, 8 pairs, one 6.4, two 8.3.
 int32_t q4_splits(const powattn_pattern* pattern, int32_t batch, int32_t hkv, int64_t capacity) {
   const int32_t mk = powattn_max_k(pattern, capacity);
