@@ -5,7 +5,7 @@
 #include "../../include/powattn.h"
 #include "pattern.h"
 
-#define POWATTN_VERSION_NUMBER 123  // 0.1.23; moves with every change to a kernel (bench.py ties its profiled traffic figures to it)
+#define POWATTN_VERSION_NUMBER 124  // 0.1.24; moves with every change to a kernel (bench.py ties its profiled traffic figures to it)
 
 // Records a HIP error for powattn_strerror and maps it to a status.
 int pa_note_hip(hipError_t e);

@@ -4,7 +4,7 @@
 // it is bound by latency and by the instructions of expanding the cache (about 430 a chunk) rather than by memory,
 // until there are enough sequences.  Keys and values are expanded to bf16 in registers, exactly (a 4-bit value
 // times a power of two is a bf16 number), and multiplied with v_mfma_f32_16x16x32_bf16.  32 query heads on 8, blocks of 64, us: one
-// sequence of 32001 tokens 6.4, 16 of 65536 7.7, 128 of 1000 .. 16384 20.7 (4.8 TB/s).
+// sequence of 32001 tokens 6.5, 16 of 65536 7.8, 128 of 1000 .. 16384 20.7 (4.8 TB/s).
 //  * A chunk is 64 tokens of a block; a wavefront requests all of one before it uses any.  Token 4i + T of it is row i of tile T
 //    (T = 0..3) of S^T = K q^T: a lane's piece of a K row lies in one scale's 32 components, the scales of its four tiles are
 //    the bytes of one word, and lane (g, q4) (g = lane % 16, q4 = lane / 16) then has the scores of tokens 16 q4 .. 16 q4 + 15.
@@ -13,8 +13,9 @@
 //  * The conversion yields two neighbouring components of a token.  For V the product wants pairs along the tokens: a token
 //    counts twice in its sum, once for each component, and P is held with zeros in the other place: O_even and O_odd are
 //    different columns.  (Bringing pairs of tokens together by byte permutes: 64 more instructions a chunk, as many products.)
-//  * P is multiplied in two parts, the upper 16 bits of its fp32 number and the upper 16 of what is left: 2^-16 off
-//    instead of bf16's 2^-9 (which would add as much again to the error of the bf16 output).  Up to 4 query heads (GM = 4): 16
+//  * P is multiplied in two parts, its nearest bf16 number and the nearest to what is left: off by at most 2^-17 of it, to either
+//    side, instead of bf16's 2^-8 (which would add as much again to the error of the bf16 output).  (Both parts cut, not rounded: one sequence
+//    6.43 us instead of 6.50, but up to 2^-15 off, always towards zero, while l_run sums P as it is.)  Up to 4 query heads (GM = 4): 16
 //    columns are 4 heads x even, odd x the two parts; up to 8 (GM = 8): two products; up to 16: four.
 //  * The wavefronts' partial (max, sum, O) meet in LDS.
 #include <math.h>
@@ -25,6 +26,7 @@
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct q4_params {
   dec_params d;                          // (k, v, packets, gen are not used)
@@ -67,6 +69,11 @@ __device__ __forceinline__ void q4_issue(q4_chunk<D>& c, const q4_params& p, int
 template <int BYTE>
 __device__ __forceinline__ float q4_scale_byte(uint32_t word) {
   return __builtin_bit_cast(float, BYTE == 3 ? word >> 1 : word << (23 - 8 * BYTE));
+}
+
+// two numbers rounded to bf16 (to the nearest, ties to even)
+__device__ __forceinline__ uint32_t q4_two(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, q4_bf16x2));
 }
 
 // A tile of scores: step s of the product is components (head_dim / 4) q4 + 8 s ..
@@ -137,25 +144,31 @@ __device__ __forceinline__ void q4_consume(q4_chunk<D>& c, const bf16x8 (&qf)[D 
   // ---- O^T += V^T P^T, 16 tokens at a time: k index 8 q4 + 2 r + parity is token 16 q4 + 4 r + T; row i of tile t is the pair of
   // components (head_dim / 16) i + 2 t, + 1 ----
   const q4_column<GM> col(g);
-  constexpr uint32_t EVEN = 0x0c0c0302u, ODD = 0x03020c0cu;      // a number's upper half in the lower half of a word, or the upper
-  const uint32_t mine = col.odd ? ODD : EVEN;
+  // of a pair of numbers, the first in the lower half of a word (even) or in the upper (odd), and the second
+  const uint32_t first = col.odd ? 0x01000c0cu : 0x0c0c0100u, second = col.odd ? 0x03020c0cu : 0x0c0c0302u;
   const float less = col.rest ? -1.f : 0.f;
   auto tokens = [&](auto tile) {
     constexpr int T = decltype(tile)::value;
     u32x4 P[GM == 4 ? 1 : GM == 8 ? 2 : 4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float x = S[T][r];
-      const float top = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+    for (int r = 0; r < 4; r += 2) {
+      const float x0 = S[T][r], x1 = S[T][r + 1];
+      const uint32_t top = q4_two(x0, x1);
+      const float top0 = __builtin_bit_cast(float, top << 16), top1 = __builtin_bit_cast(float, top & 0xffff0000u);
       if constexpr (GM == 4) {
-        const uint32_t y = __builtin_bit_cast(uint32_t, fmaf(top, less, x));
-        P[0][r] = __builtin_amdgcn_perm(y, y, mine);
+        const uint32_t y = q4_two(fmaf(top0, less, x0), fmaf(top1, less, x1));
+        P[0][r] = __builtin_amdgcn_perm(y, y, first);
+        P[0][r + 1] = __builtin_amdgcn_perm(y, y, second);
       } else {
-        const uint32_t y = __builtin_bit_cast(uint32_t, x), z = __builtin_bit_cast(uint32_t, x - top);
-        if constexpr (GM == 8) { P[0][r] = __builtin_amdgcn_perm(y, y, mine); P[1][r] = __builtin_amdgcn_perm(z, z, mine); }
-        else {
-          P[0][r] = y >> 16; P[1][r] = z >> 16;
-          P[2][r] = y & 0xffff0000u; P[3][r] = z & 0xffff0000u;
+        const uint32_t rest = q4_two(x0 - top0, x1 - top1);
+        if constexpr (GM == 8) {
+          P[0][r] = __builtin_amdgcn_perm(top, top, first); P[0][r + 1] = __builtin_amdgcn_perm(top, top, second);
+          P[1][r] = __builtin_amdgcn_perm(rest, rest, first); P[1][r + 1] = __builtin_amdgcn_perm(rest, rest, second);
+        } else {
+          P[0][r] = top & 0xffffu; P[0][r + 1] = top >> 16;
+          P[1][r] = rest & 0xffffu; P[1][r + 1] = rest >> 16;
+          P[2][r] = top << 16; P[2][r + 1] = top & 0xffff0000u;
+          P[3][r] = rest << 16; P[3][r + 1] = rest & 0xffff0000u;
         }
       }
     }
