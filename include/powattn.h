@@ -431,7 +431,8 @@ int powattn_page_tables(const powattn_pattern* pattern, const int32_t* d_q_start
  *   d_q_start         device int32 [batch] or null (zeros): row r of sequence b is position d_q_start[b] + r
  *   d_q_len           device int32 [batch] or null (all rows): rows r >= d_q_len[b] are neither read nor written
  *   q_out, k_out      device [batch, n_q_heads, rows, head_dim], [batch, n_kv_heads, rows, head_dim], contiguous, as the
- *                     attention calls take them; they may not overlap the inputs
+ *                     attention calls take them; they may not overlap q, k or one another
+ *                     (refused as INVALID_ARG)
  *   dtype             POWATTN_BF16 or POWATTN_F32; head_dim 64 or 128
  * Tensors and strides that are multiples of 16 bytes are read and written 16 bytes at a time.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP_ERROR.
@@ -446,8 +447,9 @@ int powattn_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k,
  * Gradients of sum(q_out * d_q_out) + sum(k_out * d_k_out) of powattn_qk_norm_rope with the same inputs.
  *   d_q_out, d_k_out  device, contiguous, as q_out and k_out (what powattn_backward writes as dq and dk)
  *   dq, dk            device rows with strides of their own (host int64 [3]), so that they can be written into the gradient of
- *                     the projections' output; no two rows may overlap, nor may they overlap the inputs.  Rows r >= d_q_len[b]
- *                     are not written, and nothing of theirs is read
+ *                     the projections' output; no two rows may overlap.  A call whose dq or dk shares memory with the
+ *                     other, with q, k, d_q_out or d_k_out, or whose dq_weight and dk_weight do, is refused (INVALID_ARG).
+ *                     Rows r >= d_q_len[b] are not written, and nothing of theirs is read
  *   dq_weight, dk_weight  device float [head_dim], whatever dtype is: the sums over all rows and heads, in a fixed order
  *   workspace         device, powattn_qk_norm_rope_backward_workspace_bytes(...) bytes, 256-byte aligned, contents ignored;
  *                     calls that may run at the same time must not share one

@@ -11,6 +11,7 @@
 // sixteenth of a radian); everything else is in 32 bits, rounded once at the end.
 #include <math.h>
 #include "common.h"
+#include "overlap.h"
 
 namespace {
 
@@ -385,6 +386,23 @@ int check_rotation(int32_t rot, int32_t head_dim, uint32_t flags, float eps) {
   return POWATTN_OK;
 }
 
+// Whether an output shares memory with one of the tensors that are read, or with the other output.
+bool outputs_meet(const nr_params& p, bool grad, int64_t batch, int32_t head_dim, int32_t dtype) {
+  const int32_t elem = dtype == POWATTN_F32 ? 4 : 2;
+  auto meet = [&](const void* a, const int64_t (&sa)[3], int32_t ha, const void* b, const int64_t (&sb)[3], int32_t hb) {
+    return pa_rows_meet({a, sa[0], sa[1], sa[2], ha}, {b, sb[0], sb[1], sb[2], hb}, batch, p.rows, head_dim, elem);
+  };
+  int64_t so[2][3];
+  for (int i = 0; i < 2; ++i) { so[i][0] = p.out[i].sb; so[i][1] = p.out[i].sh; so[i][2] = p.out[i].sr; }
+  for (int o = 0; o < 2; ++o)
+    for (int i = 0; i < 2; ++i) {
+      const int64_t sx[3] = {p.x[i].sb, p.x[i].sh, p.x[i].sr}, sy[3] = {p.dy[i].sb, p.dy[i].sh, p.dy[i].sr};
+      if (meet(p.out[o].p, so[o], p.heads[o], p.x[i].p, sx, p.heads[i])) return true;
+      if (grad && meet(p.out[o].p, so[o], p.heads[o], p.dy[i].p, sy, p.heads[i])) return true;
+    }
+  return meet(p.out[0].p, so[0], p.heads[0], p.out[1].p, so[1], p.heads[1]);
+}
+
 template <class T, int D, int MODE>
 void launch_forward(const nr_params& p, dim3 grid, bool inter, hipStream_t s) {
   if (inter) hipLaunchKernelGGL((pa_qk_norm_rope_kernel<T, D, MODE, true>), grid, dim3(THREADS), 0, s, p);
@@ -436,6 +454,7 @@ extern "C" int powattn_qk_norm_rope(const void* q, const int64_t* q_strides, con
   for (int i = 0; i < 2; ++i) p.out[i] = {out[i], (int64_t)p.heads[i] * rows * head_dim, rows * head_dim, head_dim};
   p.inv_freq = d_inv_freq; p.q_start = d_q_start; p.q_len = d_q_len;
   p.n_tokens = (int32_t)(batch * rows); p.rows = (int32_t)rows; p.rot = rot_dim; p.eps = eps;
+  if (outputs_meet(p, false, batch, head_dim, dtype)) return POWATTN_INVALID_ARG;
   const int64_t tok = THREADS / (head_dim / 16), groups = (p.n_tokens + tok - 1) / tok;
   deal_heads(p, groups, 1024);
   const dim3 grid((uint32_t)groups, (uint32_t)(p.chunks[0] + p.chunks[1]));
@@ -479,6 +498,9 @@ extern "C" int powattn_qk_norm_rope_backward(const void* q, const int64_t* q_str
   p.out[1] = {dk, dk_strides[0], dk_strides[1], dk_strides[2]};
   p.inv_freq = d_inv_freq; p.q_start = d_q_start; p.q_len = d_q_len;
   p.n_tokens = (int32_t)(batch * rows); p.rows = (int32_t)rows; p.rot = rot_dim; p.eps = eps;
+  if (outputs_meet(p, true, batch, head_dim, dtype)) return POWATTN_INVALID_ARG;
+  const int64_t dw_bytes = head_dim * (int64_t)sizeof(float);
+  if (pa_ranges_meet(dq_weight, dw_bytes, dk_weight, dw_bytes)) return POWATTN_INVALID_ARG;
   const nr_grid g = grad_grid(p, head_dim);
   p.partials[0] = (float*)workspace;
   p.partials[1] = p.partials[0] + (int64_t)g.x * p.chunks[0] * head_dim;
