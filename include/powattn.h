@@ -403,8 +403,8 @@ int powattn_backward(const powattn_pattern* pattern,
  *                     page is not in [0, n_pages)
  *   d_kv_len          device int32 [batch], out: s + n, as the decode calls take it
  *   d_n_taken         device int32 [1], out: the number of new pages of all sequences; more than n_free: the list was too short
- * The free list itself is not changed: the pages taken are its first d_n_taken[0].  The inputs may not overlap the
- * outputs (d_kv_len in the place of d_q_start, for instance, is refused).
+ * The free list itself is not changed: the pages taken are its first d_n_taken[0].  No output may share
+ * memory with an input or with another output (d_kv_len in the place of d_q_start, for instance): refused, INVALID_ARG.
  * Limits: table_stride * block and n_pages * block below 2^31.
  * Errors: INVALID_ARG (q_rows above table_stride*block among them), UNSUPPORTED, HIP_ERROR.
  */

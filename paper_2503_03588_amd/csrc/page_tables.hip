@@ -7,6 +7,7 @@
 // Bound by latency: a few KB are read and written (3.1 us for 128 sequences of one token, 3.8 for 32 of up to 2048).  One launch: a workgroup forms the sum over the sequences before its own
 // by itself (two words each, from L2) instead of waiting for another workgroup's.
 #include "common.h"
+#include "overlap.h"
 
 namespace {
 
@@ -112,13 +113,16 @@ extern "C" int powattn_page_tables(const powattn_pattern* pattern, const int32_t
   if (!d_q_start || !d_q_len || !d_block_table || !d_slots || !d_kv_len || !d_n_taken) return POWATTN_INVALID_ARG;
   if (batch < 1 || q_rows < 1 || n_free < 0 || n_pages < 1 || table_stride < 1) return POWATTN_INVALID_ARG;
   if (n_free > 0 && !d_free_pages) return POWATTN_INVALID_ARG;
-  // (every workgroup reads the lengths of the sequences before its own, so an output in their place would change them under it)
-  const int32_t* out[] = {d_block_table, d_slots, d_kv_len, d_n_taken};
-  for (const int32_t* o : out)
-    if (o == d_q_start || o == d_q_len || (n_free > 0 && o == d_free_pages)) return POWATTN_INVALID_ARG;
   const int64_t capacity = (int64_t)table_stride * pattern->block;
   if (q_rows > capacity) return POWATTN_INVALID_ARG;
   if (capacity > 0x7fffffff || n_pages > 0x7fffffff / pattern->block) return POWATTN_UNSUPPORTED;   // slots and positions are 32-bit numbers
+  // (every workgroup reads the lengths of the sequences before its own, so an output in their place would change them under it)
+  const struct { const void* p; int64_t bytes; } mem[] = {
+      {d_block_table, 4 * (int64_t)batch * table_stride}, {d_slots, 4 * (int64_t)batch * q_rows}, {d_kv_len, 4 * (int64_t)batch}, {d_n_taken, 4},
+      {d_q_start, 4 * (int64_t)batch}, {d_q_len, 4 * (int64_t)batch}, {d_free_pages, 4 * (int64_t)n_free}};
+  for (int o = 0; o < 4; ++o)
+    for (int i = o + 1; i < (n_free > 0 ? 7 : 6); ++i)
+      if (pa_ranges_meet(mem[o].p, mem[o].bytes, mem[i].p, mem[i].bytes)) return POWATTN_INVALID_ARG;
   pt_params p;
   p.q_start = d_q_start; p.q_len = d_q_len; p.free_pages = d_free_pages;
   p.table = d_block_table; p.slots = d_slots; p.kv_len = d_kv_len; p.n_taken = d_n_taken;

@@ -63,3 +63,26 @@ def test_gradients_that_share_memory(how):
 ])
 def test_rows_that_share_memory(how):
     assert forward(**how) == pa.INVALID_ARG
+
+
+def tables(start=MIB, n=2 * MIB, free=3 * MIB, table=4 * MIB, slots=5 * MIB, kv_len=6 * MIB, taken=7 * MIB):
+    cp = pa.Pattern(64, 4, 1).c()
+    return pa.lib().powattn_page_tables(ctypes.byref(cp), start, n, 40, 10, free, 9, 100, table, 16, slots, kv_len, taken, None)
+
+
+@pytest.mark.parametrize("how", [
+    dict(kv_len=MIB + 4),                                  # the lengths of all sequences but the first
+    dict(kv_len=MIB - 4 * 39),
+    dict(kv_len=2 * MIB + 4 * 39),
+    dict(taken=MIB + 4 * 39),
+    dict(taken=3 * MIB + 4 * 8),
+    dict(slots=2 * MIB - 4 * 399),
+    dict(table=3 * MIB - 4 * 639),
+    dict(table=3 * MIB + 4),
+    dict(kv_len=7 * MIB),                                  # one output in another
+    dict(taken=5 * MIB + 4 * 399),
+    dict(slots=4 * MIB + 4 * 639),
+    dict(kv_len=4 * MIB + 4),
+])
+def test_page_tables_that_share_memory(how):
+    assert tables(**how) == pa.INVALID_ARG
