@@ -473,7 +473,7 @@ int powattn_qk_norm_rope_backward(const void* q, const int64_t* q_strides, const
  *   k_pages, v_pages    device uint8 [n_pages, n_kv_heads, block, head_dim/2], 16-byte aligned: component 2i of a row in the
  *                       low half of byte i, 2i+1 in the high half; a code is a sign bit and the index into the list above
  *   k_scales, v_scales  device uint8 [n_pages, n_kv_heads, head_dim/32, block], 16-byte aligned: the scale codes (the token
- *                       is the fastest index)
+ *                       is the fastest index).  Where they are written, no two of the four may share memory (INVALID_ARG)
  * powattn_cache_store_q4 writes rows of keys and values at their slots:
  *   k, v                device bf16 rows [batch, n_kv_heads, rows, head_dim], strides in elements as for powattn_qk_norm_rope
  *   d_slots             device int32 [batch, rows]: page * block + offset of row r of sequence b, as powattn_page_tables
@@ -498,7 +498,8 @@ int powattn_cache_store_q4(const powattn_pattern* pattern, const void* k, const 
  *   d_start, d_length   device int32 [batch], or null (zeros, and all rows): row r of sequence b is position d_start[b] + r
  *                       for r < d_length[b], both clamped so that they stay inside the table
  *   k, v                device bf16 [batch, n_kv_heads, rows, head_dim], contiguous, 16-byte aligned; rows r >= d_length[b]
- *                       (or beyond the table) are left as they were
+ *                       (or beyond the table) are left as they were.  k and v may not share memory with one another or
+ *                       with the cache (INVALID_ARG)
  * Everything else as for powattn_cache_store_q4.
  */
 int powattn_cache_load_q4(const powattn_pattern* pattern, const void* k_pages, const void* v_pages,

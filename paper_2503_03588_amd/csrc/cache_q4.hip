@@ -7,6 +7,7 @@
 // (Four consecutive rows of a lane, of keys and values both, whose scales are one word then: stored and loaded, 32 pieces of up to 2048 rows
 // 99 / 78 us, 4000 rows of 8 heads 14.1 / 13.6, 1000 10.8 / 6.6, 128 10.4 / 4.8.)
 #include "common.h"
+#include "overlap.h"
 #include "q4.h"
 
 namespace {
@@ -119,6 +120,17 @@ int check_cache(const powattn_pattern* pattern, int32_t batch, int32_t hkv, int6
   return POWATTN_OK;
 }
 
+// Whether one of the first `n_out` pieces of memory, the outputs, shares bytes with another piece.
+struct piece { const void* p; int64_t bytes; };
+template <int N>
+bool outputs_meet(const piece (&m)[N], int n_out) {
+  for (int o = 0; o < n_out; ++o)
+    for (int i = o + 1; i < N; ++i)
+      if (pa_ranges_meet(m[o].p, m[o].bytes, m[i].p, m[i].bytes)) return true;
+  return false;
+}
+int64_t scale_bytes(int64_t n_pages, int32_t hkv, int32_t block, int32_t head_dim) { return n_pages * hkv * block * (head_dim / 32); }
+
 // As many heads of a workgroup as leave eight workgroups for every compute unit.
 bool grid_of(dim3& grid, int32_t& per_chunk, int64_t n_tokens, int32_t hkv, int32_t head_dim) {
   int n_cu = 1;
@@ -143,6 +155,8 @@ extern "C" int powattn_cache_store_q4(const powattn_pattern* pattern, const void
   if ((st = check_cache(pattern, batch, n_kv_heads, rows, n_pages, head_dim, dtype)) != POWATTN_OK) return st;
   if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)k_scales | (uintptr_t)v_scales) & 15u) return POWATTN_INVALID_ARG;
   if (((uintptr_t)k | (uintptr_t)v) & 1u) return POWATTN_INVALID_ARG;
+  const int64_t sb = scale_bytes(n_pages, n_kv_heads, pattern->block, head_dim);
+  if (outputs_meet<4>({{k_pages, 16 * sb}, {v_pages, 16 * sb}, {k_scales, sb}, {v_scales, sb}}, 4)) return POWATTN_INVALID_ARG;
   store_params p;
   p.in[0] = {(const uint16_t*)k, k_strides[0], k_strides[1], k_strides[2]};
   p.in[1] = {(const uint16_t*)v, v_strides[0], v_strides[1], v_strides[2]};
@@ -175,6 +189,8 @@ extern "C" int powattn_cache_load_q4(const powattn_pattern* pattern, const void*
   if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)k_scales | (uintptr_t)v_scales | (uintptr_t)k | (uintptr_t)v) & 15u) return POWATTN_INVALID_ARG;
   const int64_t capacity = (int64_t)table_stride * pattern->block;
   if (capacity > 0x7fffffff) return POWATTN_UNSUPPORTED;
+  const int64_t sb = scale_bytes(n_pages, n_kv_heads, pattern->block, head_dim), out = 2 * (int64_t)batch * n_kv_heads * rows * head_dim;
+  if (outputs_meet<6>({{k, out}, {v, out}, {k_pages, 16 * sb}, {v_pages, 16 * sb}, {k_scales, sb}, {v_scales, sb}}, 2)) return POWATTN_INVALID_ARG;
   load_params p;
   p.pages[0] = (const uint8_t*)k_pages; p.pages[1] = (const uint8_t*)v_pages;
   p.scales[0] = (const uint8_t*)k_scales; p.scales[1] = (const uint8_t*)v_scales;

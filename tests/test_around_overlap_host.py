@@ -86,3 +86,27 @@ def tables(start=MIB, n=2 * MIB, free=3 * MIB, table=4 * MIB, slots=5 * MIB, kv_
 ])
 def test_page_tables_that_share_memory(how):
     assert tables(**how) == pa.INVALID_ARG
+
+
+PAGES, ROWS = 16 * 2 * 64 * 64, 2 * B * HKV * N * D        # bytes of 16 pages of two heads, and of rows that are loaded
+
+
+def store(kp=MIB, vp=2 * MIB, ks=3 * MIB, vs=4 * MIB):
+    cp = pa.Pattern(64, 4, 1).c()
+    return pa.lib().powattn_cache_store_q4(ctypes.byref(cp), 5 * MIB, contiguous(HKV), 6 * MIB, contiguous(HKV), 64, kp, vp, ks, vs, 16, B, HKV,
+                                           N, D, pa.BF16, None)
+
+
+def load(kp=MIB, vp=2 * MIB, ks=3 * MIB, vs=4 * MIB, k=5 * MIB, v=6 * MIB):
+    cp = pa.Pattern(64, 4, 1).c()
+    return pa.lib().powattn_cache_load_q4(ctypes.byref(cp), kp, vp, ks, vs, 16, 64, 4, None, None, k, v, B, HKV, N, D, pa.BF16, None)
+
+
+@pytest.mark.parametrize("how", [dict(vp=MIB), dict(vp=MIB + PAGES - 16), dict(vs=3 * MIB), dict(ks=4 * MIB + PAGES // 16 - 16), dict(ks=2 * MIB + 16)])
+def test_a_cache_that_shares_memory(how):
+    assert store(**how) == pa.INVALID_ARG
+
+
+@pytest.mark.parametrize("how", [dict(v=5 * MIB), dict(v=5 * MIB + ROWS - 16), dict(k=MIB), dict(v=2 * MIB + PAGES - 16), dict(k=3 * MIB)])
+def test_loaded_rows_that_share_memory(how):
+    assert load(**how) == pa.INVALID_ARG
