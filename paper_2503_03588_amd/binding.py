@@ -213,6 +213,23 @@ def _stream(stream=None):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _made_on(stream, make, *args, **kw):
+    """A tensor that the call itself makes, on the call's stream: fills, and earlier uses of the memory, are over there before the kernel
+    writes, and what is freed when the call returns is not given to the current stream while the kernel runs.  It may be
+    used on the current stream as well (once that waits for the other)."""
+    if stream is None:
+        return make(*args, **kw)
+    here, handle = torch.cuda.current_stream(), _stream(stream)
+    if handle == here.cuda_stream:
+        return make(*args, **kw)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        t = make(*args, **kw)
+    t.record_stream(here)
+    return t
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.bfloat16:
         return BF16
@@ -288,11 +305,11 @@ def mask_build(pattern: Pattern, seq_len: int, kv_cnt=None, kv_idx=None, block_m
     nb = num_blocks(pattern, seq_len)
     if kv_idx is None:
         mk = max_k(pattern, seq_len)
-        kv_idx = torch.empty((nb, mk), dtype=torch.int32, device=device)
+        kv_idx = _made_on(stream, torch.empty, (nb, mk), dtype=torch.int32, device=device)
     if kv_cnt is None:
-        kv_cnt = torch.empty((nb,), dtype=torch.int32, device=device)
+        kv_cnt = _made_on(stream, torch.empty, (nb,), dtype=torch.int32, device=device)
     if block_mask is None and want_block_mask:
-        block_mask = torch.empty((nb, nb), dtype=torch.uint8, device=device)
+        block_mask = _made_on(stream, torch.empty, (nb, nb), dtype=torch.uint8, device=device)
     st = lib().powattn_mask_build(_pattern_ref(*pattern._values), seq_len, _ptr(kv_cnt), _ptr(kv_idx),
                                   kv_idx.shape[1], _ptr(block_mask), _stream(stream))
     _check(st, "powattn_mask_build")
@@ -313,9 +330,9 @@ def prefill(pattern: Pattern, kv_cnt, kv_idx, q, k, v, o=None, lse=None, softmax
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("q/k/v dtype mismatch")
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq, n), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq, n), dtype=torch.float32, device=q.device)
     mk = kv_idx.shape[1] if kv_idx is not None else 0
     if kv_idx is not None and kv_cnt.shape[0] * pattern.block < n:
         raise ValueError("block lists shorter than the sequence")
@@ -342,9 +359,9 @@ def prefill_chunk(pattern: Pattern, kv_cnt, kv_idx, q, k_cache, v_cache, q_start
     if k_cache.dtype != q.dtype or v_cache.dtype != q.dtype:
         raise ValueError("q/k/v dtype mismatch")
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq, q_len), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq, q_len), dtype=torch.float32, device=q.device)
     mk = kv_idx.shape[1] if kv_idx is not None else 0
     if kv_idx is not None and kv_cnt.shape[0] * pattern.block < q_start + q_len:
         raise ValueError("block lists shorter than the context")
@@ -382,9 +399,9 @@ def prefill_chunk_paged(pattern: Pattern, kv_cnt, kv_idx, q, k_pages, v_pages, b
     if kv_cnt.shape[0] * pattern.block < q_start + q_len:
         raise ValueError("block lists shorter than the context")
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq, q_len), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq, q_len), dtype=torch.float32, device=q.device)
     st = lib().powattn_prefill_chunk_paged(_pattern_ref(*pattern._values), _ptr(kv_cnt), _ptr(kv_idx), kv_idx.shape[1],
                                            _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table),
                                            block_table.shape[1], n_pages, _ptr(o), _ptr(lse),
@@ -424,9 +441,9 @@ def prefill_batch_paged(pattern: Pattern, kv_cnt, kv_idx, q, k_pages, v_pages, b
     if kv_cnt.shape[0] < block_table.shape[1]:
         raise ValueError("block lists shorter than the longest context the block table can describe")
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq, q_rows), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq, q_rows), dtype=torch.float32, device=q.device)
     st = lib().powattn_prefill_batch_paged(_pattern_ref(*pattern._values), _ptr(kv_cnt), _ptr(kv_idx), kv_idx.shape[1],
                                            _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table),
                                            block_table.shape[1], n_pages, _ptr(q_start), _ptr(q_len), q_rows,
@@ -450,11 +467,11 @@ def decode(pattern: Pattern, q, k_cache, v_cache, kv_len, o=None, lse=None, soft
     if kv_len.dtype != torch.int32 or kv_len.shape != (batch,):
         raise ValueError("kv_len must be int32 [batch]")
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq), dtype=torch.float32, device=q.device)
     if workspace is None:
-        workspace = decode_workspace(pattern, batch, hq, hkv, d, cap, q.device)
+        workspace = _made_on(stream, decode_workspace, pattern, batch, hq, hkv, d, cap, q.device)
     st = lib().powattn_decode(_pattern_ref(*pattern._values), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(kv_len),
                               cap, _ptr(o), _ptr(lse), batch, hq, hkv, d, _dtype_code(q),
                               float(softmax_scale), _ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -504,11 +521,11 @@ def decode_paged(pattern: Pattern, q, k_pages, v_pages, block_table, kv_len, o=N
         raise ValueError("kv_len must be int32 [batch]")
     stride = block_table.shape[1]
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq), dtype=torch.float32, device=q.device)
     if workspace is None:
-        workspace = decode_workspace(pattern, batch, hq, hkv, d, stride * blk, q.device)
+        workspace = _made_on(stream, decode_workspace, pattern, batch, hq, hkv, d, stride * blk, q.device)
     st = lib().powattn_decode_paged(_pattern_ref(*pattern._values), _ptr(q), _ptr(k_pages), _ptr(v_pages), n_pages,
                                     _ptr(block_table), stride, _ptr(kv_len), _ptr(o), _ptr(lse),
                                     batch, hq, hkv, d, _dtype_code(q), float(softmax_scale),
@@ -542,16 +559,16 @@ def backward(pattern: Pattern, kv_cnt, kv_idx, q, k, v, o, lse, d_o, dq=None, dk
         if t.dtype != q.dtype:
             raise ValueError("dtype mismatch")
     if dq is None:
-        dq = torch.empty_like(q)
+        dq = _made_on(stream, torch.empty_like, q)
     if dk is None:
-        dk = torch.empty_like(k)
+        dk = _made_on(stream, torch.empty_like, k)
     if dv is None:
-        dv = torch.empty_like(v)
+        dv = _made_on(stream, torch.empty_like, v)
     if workspace is None:
         need = backward_workspace_bytes(pattern, batch, hq, hkv, n, d)
         if need == 0:
             raise PowattnError(INVALID_ARG, "powattn_backward_workspace_bytes")
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _made_on(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     st = lib().powattn_backward(_pattern_ref(*pattern._values), _ptr(kv_cnt), _ptr(kv_idx), kv_idx.shape[1],
                                 _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv),
                                 batch, hq, hkv, n, d, _dtype_code(q), float(softmax_scale),
@@ -579,9 +596,9 @@ def prefill_varlen(pattern: Pattern, kv_cnt, kv_idx, q, k, v, seq_lens, o=None, 
     if kv_idx is not None and kv_cnt.shape[0] * pattern.block < npad:
         raise ValueError("block lists shorter than the padded length")
     if o is None:
-        o = torch.zeros_like(q)
+        o = _made_on(stream, torch.zeros_like, q)
     if lse is None and want_lse:
-        lse = torch.zeros((batch, hq, npad), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.zeros, (batch, hq, npad), dtype=torch.float32, device=q.device)
     mk = kv_idx.shape[1] if kv_idx is not None else 0
     st = lib().powattn_prefill_varlen(_pattern_ref(*pattern._values), _ptr(kv_cnt), _ptr(kv_idx), mk,
                                       _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), batch, hq, hkv, _ptr(seq_lens),
@@ -641,11 +658,11 @@ def page_tables(pattern: Pattern, q_start, q_len, free_pages, block_table, n_pag
         raise ValueError("block_table must be int32 [batch, table_stride]")
     _int32("block_table", block_table, (batch, block_table.shape[1]))
     if slots is None:
-        slots = torch.empty((batch, q_rows), dtype=torch.int32, device=q_start.device)
+        slots = _made_on(stream, torch.empty, (batch, q_rows), dtype=torch.int32, device=q_start.device)
     if kv_len is None:
-        kv_len = torch.empty((batch,), dtype=torch.int32, device=q_start.device)
+        kv_len = _made_on(stream, torch.empty, (batch,), dtype=torch.int32, device=q_start.device)
     if n_taken is None:
-        n_taken = torch.empty((1,), dtype=torch.int32, device=q_start.device)
+        n_taken = _made_on(stream, torch.empty, (1,), dtype=torch.int32, device=q_start.device)
     _int32("slots", slots, (batch, q_rows))
     _int32("kv_len", kv_len, (batch,))
     _int32("n_taken", n_taken, (1,))
@@ -688,9 +705,9 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, q_start=None, q_len=None, e
     strides, (batch, hq, hkv, rows, d), rot = _rope_arguments(q, k, q_weight, k_weight, inv_freq, q_start, q_len)
     new = torch.empty if q_len is None else torch.zeros
     if q_out is None:
-        q_out = new((batch, hq, rows, d), dtype=q.dtype, device=q.device)
+        q_out = _made_on(stream, new, (batch, hq, rows, d), dtype=q.dtype, device=q.device)
     if k_out is None:
-        k_out = new((batch, hkv, rows, d), dtype=q.dtype, device=q.device)
+        k_out = _made_on(stream, new, (batch, hkv, rows, d), dtype=q.dtype, device=q.device)
     _output("q_out", q_out, (batch, hq, rows, d), q.dtype)
     _output("k_out", k_out, (batch, hkv, rows, d), q.dtype)
     _on_this_gpu(q_out, k_out)
@@ -728,22 +745,22 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, inv_freq, dq_out, dk_out, q_
     _output("dk_out", dk_out, (batch, hkv, rows, d), q.dtype)
     new = torch.empty if q_len is None else torch.zeros
     if dq is None:
-        dq = new((batch, hq, rows, d), dtype=q.dtype, device=q.device)
+        dq = _made_on(stream, new, (batch, hq, rows, d), dtype=q.dtype, device=q.device)
     if dk is None:
-        dk = new((batch, hkv, rows, d), dtype=q.dtype, device=q.device)
+        dk = _made_on(stream, new, (batch, hkv, rows, d), dtype=q.dtype, device=q.device)
     grad_strides = _rows("dq", dq), _rows("dk", dk)
     if dq.shape != q.shape or dk.shape != k.shape or dq.dtype != q.dtype or dk.dtype != q.dtype:
         raise ValueError("dq/dk must have the shapes and the type of q/k")
     _rows_apart("dq", dq)
     _rows_apart("dk", dk)
     if dq_weight is None:
-        dq_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+        dq_weight = _made_on(stream, torch.empty, (d,), dtype=torch.float32, device=q.device)
     if dk_weight is None:
-        dk_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+        dk_weight = _made_on(stream, torch.empty, (d,), dtype=torch.float32, device=q.device)
     _output("dq_weight", dq_weight, (d,), torch.float32)
     _output("dk_weight", dk_weight, (d,), torch.float32)
     if workspace is None:
-        workspace = qk_norm_rope_backward_workspace(batch, hq, hkv, rows, d, q.device)
+        workspace = _made_on(stream, qk_norm_rope_backward_workspace, batch, hq, hkv, rows, d, q.device)
     _on_this_gpu(dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace)
     st = lib().powattn_qk_norm_rope_backward(
         q.data_ptr(), strides[0], k.data_ptr(), strides[1], _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), rot,
@@ -815,9 +832,9 @@ def cache_load_q4(pattern: Pattern, cache, block_table, rows: int, start=None, l
             _int32(name, t, (batch,))
     pages, n_pages = _cache_q4(pattern, cache, hkv, d)
     if k is None:
-        k = torch.zeros((batch, hkv, rows, d), dtype=torch.bfloat16, device=block_table.device)
+        k = _made_on(stream, torch.zeros, (batch, hkv, rows, d), dtype=torch.bfloat16, device=block_table.device)
     if v is None:
-        v = torch.zeros((batch, hkv, rows, d), dtype=torch.bfloat16, device=block_table.device)
+        v = _made_on(stream, torch.zeros, (batch, hkv, rows, d), dtype=torch.bfloat16, device=block_table.device)
     _output("k", k, (batch, hkv, rows, d), torch.bfloat16)
     _output("v", v, (batch, hkv, rows, d), torch.bfloat16)
     _on_this_gpu(block_table, start, length, k, v)
@@ -859,14 +876,14 @@ def decode_paged_q4(pattern: Pattern, q, cache, block_table, kv_len, o=None, lse
     _int32("kv_len", kv_len, (batch,))
     pages, n_pages = _cache_q4(pattern, cache, hkv, d)
     if o is None:
-        o = torch.empty_like(q)
+        o = _made_on(stream, torch.empty_like, q)
     if lse is None and want_lse:
-        lse = torch.empty((batch, hq), dtype=torch.float32, device=q.device)
+        lse = _made_on(stream, torch.empty, (batch, hq), dtype=torch.float32, device=q.device)
     _output("o", o, q.shape, q.dtype)
     if lse is not None:
         _output("lse", lse, (batch, hq), torch.float32)
     if workspace is None:
-        workspace = decode_paged_q4_workspace(pattern, batch, hq, hkv, d, stride * pattern.block, q.device)
+        workspace = _made_on(stream, decode_paged_q4_workspace, pattern, batch, hq, hkv, d, stride * pattern.block, q.device)
     _on_this_gpu(q, block_table, kv_len, o, lse, workspace)
     st = lib().powattn_decode_paged_q4(_pattern_ref(*pattern._values), _ptr(q), *pages, n_pages, _ptr(block_table), stride,
                                        _ptr(kv_len), _ptr(o), _ptr(lse), batch, hq, hkv, d, _dtype_code(q),
