@@ -39,6 +39,15 @@ class pa_rows_trial {
  public:
   bool meet(const pa_rows& a, const pa_rows& b, int64_t batch, int64_t rows, int32_t head_dim, int32_t elem, int most) {
     const int64_t sa[3] = {a.sb, a.sh, a.sr}, sb[3] = {b.sb, b.sh, b.sr}, na[3] = {batch, a.heads, rows}, nb[3] = {batch, b.heads, rows};
+    const int64_t delta = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+    row = (int64_t)head_dim * elem;
+    int64_t least = delta, farthest = delta;               // memory that is apart altogether: most calls
+    for (int i = 0; i < 3; ++i) {
+      const int64_t x = (1 - na[i]) * sa[i] * elem, y = (nb[i] - 1) * sb[i] * elem;
+      least += std::min<int64_t>(x, 0) + std::min<int64_t>(y, 0);
+      farthest += std::max<int64_t>(x, 0) + std::max<int64_t>(y, 0);
+    }
+    if (least >= row || farthest <= -row) return false;
     for (int i = 0; i < 3; ++i) {
       if (sa[i] == sb[i]) add(sa[i] * elem, 1 - na[i], nb[i] - 1);
       else { add(sa[i] * elem, 1 - na[i], 0); add(sb[i] * elem, 0, nb[i] - 1); }
@@ -46,9 +55,8 @@ class pa_rows_trial {
     std::sort(d, d + n, [](const dim& x, const dim& y) { return x.step > y.step; });
     lo[n] = hi[n] = 0;
     for (int i = n - 1; i >= 0; --i) { lo[i] = lo[i + 1] + d[i].step * d[i].lo; hi[i] = hi[i + 1] + d[i].step * d[i].hi; }
-    row = (int64_t)head_dim * elem;
     left = most;
-    return from(0, (int64_t)((uintptr_t)b.p - (uintptr_t)a.p));
+    return from(0, delta);
   }
 };
 inline bool pa_rows_meet(const pa_rows& a, const pa_rows& b, int64_t batch, int64_t rows, int32_t head_dim, int32_t elem, int most = 1 << 14) {
