@@ -3,7 +3,8 @@
 // Both move bytes and nothing else.  A lane has 8 components, 16 bytes in bf16 and 4 in the cache, four lanes share a scale, and a
 // wavefront takes consecutive rows, so that its pieces of a page are one stretch.  A workgroup looks its rows' slots (pages)
 // up once and walks through heads; the next head's rows are requested before the current one's are converted.
-// 37399 rows of 8 heads of 128: stored in 36.6 us (5.3 TB/s), loaded in 34.7 (5.6); 128 rows 3.3 and 3.2.
+// 34352 and 37399 rows of 8 heads of 128 in turn: stored in 43.7 us (4.3 TB/s), loaded in 33.7 (5.5); the same 37399 rows again and again: stored
+// in 36.6 (5.3); 128 rows 3.0 and 2.8.  Whole contexts, 8 of 16384 tokens, loaded cold: 143 us with the launch (4.7 TB/s).
 // (Four consecutive rows of a lane, of keys and values both, whose scales are one word then: stored and loaded, 32 pieces of up to 2048 rows
 // 99 / 78 us, 4000 rows of 8 heads 14.1 / 13.6, 1000 10.8 / 6.6, 128 10.4 / 4.8.)
 #include "common.h"

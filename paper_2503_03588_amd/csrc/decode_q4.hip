@@ -3,8 +3,9 @@
 // A step reads 2 * (head_dim / 2 + head_dim / 32) bytes per attended token and KV head, 0.27 of the bf16 step's, so that
 // it is bound by latency and by the instructions of expanding the cache (about 430 a chunk) rather than by memory,
 // until there are enough sequences.  Keys and values are expanded to bf16 in registers, exactly (a 4-bit value
-// times a power of two is a bf16 number), and multiplied with v_mfma_f32_16x16x32_bf16.  32 query heads on 8, blocks of 64, us: one
-// sequence of 32001 tokens 6.5, 16 of 65536 7.8, 128 of 1000 .. 16384 20.7 (4.8 TB/s).
+// times a power of two is a bf16 number), and multiplied with v_mfma_f32_16x16x32_bf16.  us, blocks of 64, from a graph, one
+// sequence of 32001 tokens / 16 of 65536 / 128 of 1000 .. 16384: 32 query heads on 8 6.5 / 7.8 / 20.7 (4.3 TB/s), 28 on 4 (GM = 8) 6.9 /
+// 8.0 / 13.4, 64 on 4 (GM = 16) - / - / 18.5; 32 on 8, blocks of 256, 64 of 10000 .. 30000: 34 (4.8 TB/s).
 //  * A chunk is 64 tokens of a block; a wavefront requests all of one before it uses any.  Token 4i + T of it is row i of tile T
 //    (T = 0..3) of S^T = K q^T: a lane's piece of a K row lies in one scale's 32 components, the scales of its four tiles are
 //    the bytes of one word, and lane (g, q4) (g = lane % 16, q4 = lane / 16) then has the scores of tokens 16 q4 .. 16 q4 + 15.

@@ -7,8 +7,9 @@
 // Reason: the smallest calls take 8 to 12 us on the GPU, and marshalling them in Python took 6 to 8 us each (tensor
 // attributes, shapes, ctypes); now 3.5 to 5.  A list and a prefill of 1024 fp32 queries, two calls, were paced by it: 16.2 us
 // -> 12.0; a call that is waited for: one decode step 21.7 -> 18.6 us, a chunk 46.3 -> 42.7, list and prefill 32.8 -> 25.6.
-// The calls around the attention have more arguments to look at: pages and slots of 128 sequences 11.1 -> 4.5 us, norm and
-// rotation of 2 x 1000 rows 15.0 -> 4.9, its gradients (2 x 777) 29.8 -> 9.2, a whole decode step of 64 sequences 54 -> 35.
+// The calls around the attention have more arguments to look at, us a pass, marshalled in Python -> here: pages and slots of 128
+// sequences 11.5 -> 5.2, norm and rotation of 2 x 1000 rows 15.4 -> 5.5, its gradients (2 x 777) 30.3 -> 10.5 (the GPU's time), 128 rows stored and
+// loaded 26.8 -> 8.7, a whole decode step of 64 sequences 52.5 -> 23.9 (the GPU's time).
 #include <algorithm>
 #include <array>
 #include <initializer_list>

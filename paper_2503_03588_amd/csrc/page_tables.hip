@@ -4,8 +4,9 @@
 // number sum over the sequences before it of their new pages.  A new page's first token is one of the n (its block starts at
 // s or later), so the thread of that token enters it into the table, and every token's slot is page * B + offset.
 //
-// Bound by latency: a few KB are read and written (3.1 us for 128 sequences of one token, 3.8 for 32 of up to 2048).  One launch: a workgroup forms the sum over the sequences before its own
-// by itself (two words each, from L2) instead of waiting for another workgroup's.
+// Bound by latency: a few KB are read and written (3.1 us for 128 sequences of one token, 4.3 for 32 of up to 2048).
+// One launch: a workgroup forms the sum over the sequences before its own by itself (two words each, from L2) instead of
+// waiting for another workgroup's.
 #include "common.h"
 #include "overlap.h"
 

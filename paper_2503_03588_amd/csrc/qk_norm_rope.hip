@@ -190,7 +190,8 @@ __global__ __launch_bounds__(THREADS) void pa_qk_norm_rope_kernel(nr_params p) {
       nr_load<VEC>(v[i], x + (h + i) * xh + at.b);
     }
   };
-  request(ra, rb, h0);                     // (under way while the angles are formed)
+  // (under way while the angles are formed; with a q_start the angles wait for it, and thereby for the rows requested before it)
+  request(ra, rb, h0);
   nr_angles(cs, sn, turns, (int64_t)(p.q_start ? p.q_start[b] : 0) + r);
   float w0[8], w1[8];
   nr_floats(w0, wa);
